@@ -41,7 +41,8 @@ enum {
   FGATTN_E_DEVICE = -7,      /* not a gfx950 device, or a HIP runtime call failed */
   FGATTN_E_MASK = -8,        /* fgattn_validate_mask found a bad mask */
   FGATTN_E_FLAGS = -9,       /* unknown flag bits */
-  FGATTN_E_STATIC_LIMIT = -10 /* fgattn_forward_static: more work items than FGATTN_STATIC_MAX_ITEMS */
+  FGATTN_E_STATIC_LIMIT = -10, /* fgattn_forward_static: more work items than FGATTN_STATIC_MAX_ITEMS */
+  FGATTN_E_DTYPE = -11       /* a tensor of a type that the call does not take */
 };
 
 enum {
@@ -210,6 +211,129 @@ const char* fgattn_strerror(int code);
 #define FGATTN_STATIC_MAX_ITEMS 65536
 int fgattn_forward_static(const void* q, const void* k, const void* v, const int64_t* mask_indptr,
                           const int32_t* mask_indices, const fgattn_params* p, void* out, float* lse, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Around the sparse attention of a layer: rotary positions and per-head norms of queries and keys (the step before the
+ * mask and the forward pass).  Same conventions as above: device pointers unless said otherwise, strides in
+ * elements, asynchronous on `stream`, no allocation, the same bits every time, FGATTN_* codes.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+enum { FGATTN_BF16 = 0, FGATTN_FP16 = 1, FGATTN_FP32 = 2 };   /* types of tensor elements */
+
+/* One axis of the token grid (e.g. time, height, width; or the sequence itself) and the pairs of a head that it turns. */
+typedef struct fgattn_rope_axis {
+  int32_t size;        /* positions along the axis, >= 1 */
+  int32_t pairs;       /* pairs of elements of a head that turn with it, >= 1 */
+  double theta;        /* pair j turns by theta^(-j / pairs) per position; > 0 */
+  double offset, step; /* position of coordinate x: offset + step * x */
+  double factor;       /* context extension, > 0; 1 = none */
+  double original;     /* trained length; 0: every pair turns 1/factor as fast (positions interpolated) */
+  double beta_fast, beta_slow;   /* original > 0: pairs that turn at least beta_fast times over the trained length keep
+                                    their speed, those that turn at most beta_slow times turn 1/factor as fast, and
+                                    between the two the share kept grows linearly; beta_fast > beta_slow */
+} fgattn_rope_axis;
+
+/*
+ * Table of the rotary angles of a token grid: row l = the token with coordinates (x_0, .., x_{n-1}) = l unravelled with the
+ * last axis fastest; columns = the pairs of axis 0, then of axis 1, ..  cos and sin: fp32 [rows, pairs], contiguous,
+ * written with mscale * cos(angle) and mscale * sin(angle) (formed in 64 bits, rounded once).
+ *   axes : HOST array of n_axes (1 .. 3) axes; rows = the product of the sizes, <= 2^24; the pairs sum to at most 128.
+ * Errors: FGATTN_E_SHAPE for sizes out of range, FGATTN_E_SCALE for numbers that are not finite or not as above.
+ */
+int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, float mscale, float* cos, float* sin, void* stream);
+
+enum { FGATTN_ROPE_INTERLEAVED = 0,   /* pair j of a head = its elements 2j and 2j + 1 */
+       FGATTN_ROPE_HALF = 1 };        /* pair j = elements j and j + rot_dims / 2 */
+enum { FGATTN_FLAG_ROPE_NORM = 1,           /* RMS norm of every row (one head of one token) ahead of the rotation */
+       FGATTN_FLAG_ROPE_WEIGHT_FP32 = 2 };  /* the norm weights are fp32 whatever `dtype` is (otherwise of that type) */
+
+typedef struct fgattn_rope_params {
+  int32_t B, Hq, Hk, L, d;       /* batch, heads of q and of k (0: no k), tokens (<= 2^24), head dim: a multiple of 8, 8 .. 256 */
+  int32_t rot_dims;              /* elements of a head that are turned, from its first on: even, 0 .. d */
+  int32_t layout;                /* FGATTN_ROPE_* */
+  int32_t dtype;                 /* type of q, k and of the results */
+  int32_t flags;                 /* FGATTN_FLAG_ROPE_* */
+  float eps;                     /* added to the mean square; finite, >= 0 */
+  /* strides in ELEMENTS, multiples of 8, the last dimension contiguous; q, k: the inputs (and, backward, their gradients);
+   * qo, ko: the results (backward: the gradients that come in) */
+  int64_t q_stride_b, q_stride_h, q_stride_l;
+  int64_t k_stride_b, k_stride_h, k_stride_l;
+  int64_t qo_stride_b, qo_stride_h, qo_stride_l;
+  int64_t ko_stride_b, ko_stride_h, ko_stride_l;
+} fgattn_rope_params;
+
+/*
+ * Queries and keys, normed per head and turned by their positions, in one pass:
+ *   z = x * rsqrt(mean(x^2) + eps) * weight  (with FGATTN_FLAG_ROPE_NORM, else z = x);
+ *   (y_a, y_b) = (z_a cos - z_b sin, z_b cos + z_a sin) for every pair (a, b), y = z for the elements from rot_dims on.
+ * Formed in fp32, rounded once.
+ *   q, k        : [B, Hq, L, d] and [B, Hk, L, d] (k may be NULL where Hk = 0), 16-byte aligned.
+ *   q_weight, k_weight : [d] or NULL (weight 1); NULL without the norm flag.
+ *   cos, sin    : fp32 [table_rows, rot_dims / 2], contiguous (fgattn_rope_table's, or any); NULL allowed where rot_dims = 0.
+ *   positions   : int32 [B, L], the table's row of every token; NULL: token l takes row l, and table_rows >= L.  A position
+ *                 outside [0, table_rows) turns nothing (as angle 0 and mscale 1 would): padding may hold -1.
+ *   q_out, k_out: the results; each may be its input itself (same strides).
+ */
+int fgattn_rope_forward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,
+                        const float* sin, int32_t table_rows, const int32_t* positions, const fgattn_rope_params* p,
+                        void* q_out, void* k_out, void* stream);
+
+/*
+ * Its gradients.  With the gradients dq_out, dk_out of the results (strides qo, ko): dq, dk (strides q, k; each may be the
+ * incoming gradient itself where strides agree) and, with the norm flag, dq_weight, dk_weight: fp32 [d], summed over all
+ * rows (each may be NULL: not wanted).  q, k: the forward call's inputs; without the norm flag they are not read and may
+ * be NULL.  `workspace` (>= fgattn_rope_workspace_bytes(p), 256-byte aligned) may be NULL where no weight gradient is
+ * wanted.
+ */
+size_t fgattn_rope_workspace_bytes(const fgattn_rope_params* p);
+int fgattn_rope_backward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,
+                         const float* sin, int32_t table_rows, const int32_t* positions, const fgattn_rope_params* p,
+                         const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Cross attention: the layer's tokens attend to another sequence (an encoder's states) of its own length.
+ * --------------------------------------------------------------------------------------------------------------- */
+typedef struct fgattn_cross_params {
+  int32_t B, H, Hkv;             /* batch, query heads, key heads: H a multiple of Hkv, query head h reads key head h / (H / Hkv) */
+  int32_t Lq, Lk, d;             /* query tokens and keys (each <= 2^24), head dim (64 or 128) */
+  /* strides in ELEMENTS (bf16), as in fgattn_params; the last four are read by the backward call only */
+  int64_t q_stride_b, q_stride_h, q_stride_l;
+  int64_t k_stride_b, k_stride_h, k_stride_l;
+  int64_t v_stride_b, v_stride_h, v_stride_l;
+  int64_t o_stride_b, o_stride_h, o_stride_l;
+  int64_t do_stride_b, do_stride_h, do_stride_l;
+  int64_t dq_stride_b, dq_stride_h, dq_stride_l;
+  int64_t dk_stride_b, dk_stride_h, dk_stride_l;
+  int64_t dv_stride_b, dv_stride_h, dv_stride_l;
+  float scale;                   /* multiplies Q K^T */
+  int32_t flags;                 /* 0 */
+} fgattn_cross_params;
+
+/*
+ * out = softmax(scale * Q K^T) V over the first k_lens[b] keys, lse = ln sum exp(scale * q.k) over them.
+ *   q, out : bf16 [B, H, Lq, d];  k, v : bf16 [B, Hkv, Lk, d];  lse : fp32 [B, H, Lq] contiguous.
+ *   q_lens, k_lens : int32 [B] or NULL (all tokens / all keys); values are taken into [0, Lq] and [0, Lk].
+ *            Keys from k_lens[b] on are not read, whatever they hold; rows of out and lse from q_lens[b] on are not written.
+ *            No keys: out = 0, lse = -inf.
+ * `workspace`: at least fgattn_cross_workspace_bytes(p) bytes, 256-byte aligned; NULL where that is 0.  (Calls with few rows
+ * split the keys over the chip and join the parts there.)
+ */
+size_t fgattn_cross_workspace_bytes(const fgattn_cross_params* p);
+int fgattn_cross_forward(const void* q, const void* k, const void* v, const int32_t* q_lens, const int32_t* k_lens,
+                         const fgattn_cross_params* p, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/*
+ * Its gradients: dq, dk, dv (bf16, every element written: zeros for rows from q_lens[b] and keys from k_lens[b] on) from
+ * the forward call's inputs and results and dout, the gradient of out (rows from q_lens[b] on are not read, of out and
+ * lse neither).  Where query heads share a key head its gradient is the sum of theirs.  P and dS are rounded to
+ * bf16 for the matrix instructions, all sums are fp32, the results are rounded once.
+ */
+size_t fgattn_cross_backward_workspace_bytes(const fgattn_cross_params* p);
+int fgattn_cross_backward(const void* q, const void* k, const void* v, const void* out, const float* lse, const void* dout,
+                          const int32_t* q_lens, const int32_t* k_lens, const fgattn_cross_params* p, void* dq, void* dk,
+                          void* dv, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------------------
  * Measurement aids -- not part of the method, not needed by any caller of the path; benchmarks use them.

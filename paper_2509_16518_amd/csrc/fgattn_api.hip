@@ -151,6 +151,13 @@ static int device_info(DeviceInfo* out) {
   return d.gfx950 ? FGATTN_OK : FGATTN_E_DEVICE;
 }
 
+int require_device(int* cus) {
+  DeviceInfo dev;
+  const int rc = device_info(&dev);
+  if (rc == FGATTN_OK && cus != nullptr) *cus = dev.cus;
+  return rc;
+}
+
 static int64_t n_items_of(const fgattn_params* p) {
   return (int64_t)p->B * p->H * (((int64_t)p->L + p->M - 1) / p->M);
 }
@@ -453,6 +460,7 @@ const char* fgattn_strerror(int code) {
     case FGATTN_E_MASK: return "mask failed validation";
     case FGATTN_E_FLAGS: return "unknown flag bits";
     case FGATTN_E_STATIC_LIMIT: return "fgattn_forward_static: more work items than FGATTN_STATIC_MAX_ITEMS";
+    case FGATTN_E_DTYPE: return "a tensor of a type that the call does not take";
     default: return "unknown fgattn error code";
   }
 }

@@ -40,7 +40,18 @@ struct FwdArgs {
   const int32_t* group_tiles;   // [n_items * R] member tile ids inside the slice, -1 = no tile
   const uint8_t* memb;          // [nnz of the union lists] member bit masks
   int32_t tile_rows, R;
+  // cross attention: H = key heads, L = query rows that share a key head (the heads of its group one below the other, Lq
+  // each), M = rows of the launched tile, Lk = keys; an item is a tile of rows against one of n_split ranges of
+  // split_keys keys, and with several its unnormalised result goes to part_o [item][M][d] and part_ml [item][M][2]
+  const int32_t* q_lens;        // [B] or null
+  const int32_t* k_lens;        // [B] or null
+  float* part_o;
+  float* part_ml;
+  int32_t Lq, Lk, group, n_split, split_keys;
 };
+
+// FGATTN_OK if the current device is a gfx950 (its compute units in *cus, which may be null), else FGATTN_E_DEVICE.
+int require_device(int* cus);
 
 // Launches the forward kernel variant for (a.M, d) on `stream` with a persistent grid sized to
 // the device (`cus` compute units).  If grid_only != nullptr nothing is launched and the grid

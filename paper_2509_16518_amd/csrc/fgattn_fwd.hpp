@@ -188,7 +188,8 @@ __device__ __forceinline__ float row_max(const f32x16& S) {
 //   NMODE_GROUPS  N >= 1 keys per group: key = indices[position / N] * N + position % N, L a multiple of N;
 //   NMODE_GROUPS_SHORT  the same with a short last group (L not a multiple of N): any tile may then hold
 //                 positions past the end of the sequence, which are masked out.
-enum { NMODE_DENSE = 0, NMODE_N1 = 1, NMODE_GROUPS = 2, NMODE_GROUPS_SHORT = 3 };
+//   NMODE_CROSS   position == key of another sequence, with its own length per batch entry: see fgcross_fwd.hip.
+enum { NMODE_CROSS = -1, NMODE_DENSE = 0, NMODE_N1 = 1, NMODE_GROUPS = 2, NMODE_GROUPS_SHORT = 3 };
 
 // PART selects what is executed: PART_ALL is the forward pass; PART_GATHER keeps only the index translation and
 // the row gathers, PART_COMPUTE everything but the row gathers (both leave meaningless results and exist so that
@@ -242,7 +243,8 @@ template <int MT, int D, int NMODE, int OCC, int PART = PART_ALL, bool GROUPED =
           bool DENSE_PRIO = false>
 __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs a) {
   using C = FwdCfg<MT, D, KS, VS, WV>;
-  constexpr bool DENSE = NMODE == NMODE_DENSE;
+  constexpr bool CROSS = NMODE == NMODE_CROSS;
+  constexpr bool DENSE = NMODE == NMODE_DENSE || CROSS;
   constexpr bool WAVE_PRIO = DENSE ? DENSE_PRIO : NMODE == NMODE_N1 || MT > 32;
   constexpr bool SHORT_GROUP = NMODE == NMODE_GROUPS_SHORT;   // (the host picks the variant from L % N)
   // the cross-lane permute of the ids is issued before the barrier that precedes its use (measured with one key per group:
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
 
   const int tid = threadIdx.x;
   // without a pre-pass, what it leaves in the workspace is written here: cleared control words and an order
-  if (a.schedule == SCHED_DIRECT) {
+  if (!CROSS && a.schedule == SCHED_DIRECT) {
     if (blockIdx.x == 0 && tid < 64) a.counter[tid] = 0;
     if (a.leave_order && tid == 0) a.order[blockIdx.x] = blockIdx.x;
   }
@@ -341,6 +343,12 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
   bool home_dry = false;
   for (;;) {
     // ---------------- fetch the next work item ----------------
+    int w;
+    if constexpr (CROSS) {   // one item per workgroup, a contiguous eighth of the items per XCD
+      const int r = blockIdx.x & 7, per = a.n_items >> 3, rem = a.n_items & 7;
+      if (iter++ > 0) break;
+      w = r * per + min(r, rem) + (blockIdx.x >> 3);
+    } else {
     if (tid == 0) {
       int item = -1;
       if (a.schedule == SCHED_DIRECT) {   // at most one item per workgroup; a contiguous eighth of the items per XCD
@@ -374,11 +382,13 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
     }
     iter++;
     __syncthreads();
-    const int w = __builtin_amdgcn_readfirstlane(*s_item);
+    w = __builtin_amdgcn_readfirstlane(*s_item);
     __syncthreads();   // the word lies inside the tile ring: every wave has read it before any gather may land there
     if (w < 0) break;
+    }
 
-    const int slice = w / a.QB, qi = w - slice * a.QB;
+    const int tile_item = CROSS ? w / a.n_split : w;
+    const int slice = tile_item / a.QB, qi = tile_item - slice * a.QB;
     const int b = slice / a.H, h = slice - b * a.H;
     const int row0 = qi * a.M;
     const int row_end = min(row0 + a.M, a.L);
@@ -393,9 +403,24 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
       my_row = tile * a.tile_rows + (qg - my_member * a.tile_rows);
       my_row_valid = tile >= 0 && my_row < a.L;
     }
+    int my_head = h, my_pos = my_row;   // CROSS: this lane's query head and token
+    int key0 = 0;                       // CROSS: the first key of the item's range
+    if constexpr (CROSS) {
+      const int row = min(my_row, a.L - 1), of_group = (int)((unsigned)row / (unsigned)a.Lq);
+      my_head = h * a.group + of_group;
+      my_pos = row - of_group * a.Lq;
+      const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
+      my_row_valid &= my_pos < q_len;
+      const int first_of = row0 / a.Lq;   // (an item of nothing but rows past the end of its sequence)
+      if (first_of == (row_end - 1) / a.Lq && row0 - first_of * a.Lq >= q_len) break;
+    }
     int64_t beg = 0;
     int cnt;  // active key groups of this item
-    if (DENSE) {
+    if constexpr (CROSS) {
+      const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+      key0 = (w - tile_item * a.n_split) * a.split_keys;
+      cnt = max(0, min(k_len - key0, a.split_keys));
+    } else if (DENSE) {
       cnt = a.L;
     } else {
       beg = a.indptr[w];
@@ -405,14 +430,15 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
     const int ntiles = (total + C::NT - 1) / C::NT;
     // (wave-uniform; pinned to scalar registers here, an item's set-up ahead of the first id load that uses it as its base)
     const int32_t* idx = DENSE ? nullptr : static_cast<const int32_t*>(pin_scalar(a.indices + beg));
-    const uint16_t* kbase = a.k + b * a.k_sb + h * a.k_sh;
-    const uint16_t* vbase = a.v + b * a.v_sb + h * a.v_sh;
+    const uint16_t* kbase = a.k + b * a.k_sb + h * a.k_sh + key0 * a.k_sl;
+    const uint16_t* vbase = a.v + b * a.v_sb + h * a.v_sh + key0 * a.v_sl;
 
     // ---------------- Q fragment (B operand of S^T), once per item ----------------
     bf16x8 qf[C::SSTEPS];
     {
       int qrow = GROUPED ? (my_row_valid ? my_row : 0) : min(my_row, a.L - 1);
-      const char* qp = reinterpret_cast<const char*>(a.q + b * a.q_sb + h * a.q_sh + (int64_t)qrow * a.q_sl);
+      if constexpr (CROSS) qrow = my_pos;
+      const char* qp = reinterpret_cast<const char*>(a.q + b * a.q_sb + (CROSS ? my_head : h) * a.q_sh + (int64_t)qrow * a.q_sl);
 #pragma unroll
       for (int s = 0; s < C::SSTEPS; s++) {
         i32x4 raw = *reinterpret_cast<const i32x4*>(qp + (2 * s + g) * 16);
@@ -494,7 +520,7 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
     auto spread = [&](int T, int key, int (&dst)[C::IPW]) {
 #pragma unroll
       for (int i = 0; i < C::IPW; i++) {
-        if constexpr (DENSE) dst[i] = min(T * C::NT + lpos + i * C::RPI, a.L - 1);
+        if constexpr (DENSE) dst[i] = min(T * C::NT + lpos + i * C::RPI, (CROSS ? cnt : a.L) - 1);
         else dst[i] = __builtin_amdgcn_ds_bpermute((i * C::RPI + lrow) << 2, key);
       }
     };
@@ -943,9 +969,29 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
     }
     if (kw == 0) {
       const int row = my_row;
+      if constexpr (CROSS) {
+        if (a.n_split > 1) {   // a part of the row's keys: joined with the others by a kernel of its own
+          if (my_row_valid) {
+            const int64_t at = (int64_t)w * MT + rw * 32 + ln;
+            float* op = a.part_o + at * D;
+#pragma unroll
+            for (int db = 0; db < C::DBLK; db++)
+#pragma unroll
+              for (int r4 = 0; r4 < 4; r4++) {
+                const f32x4 f = {O[db][4 * r4], O[db][4 * r4 + 1], O[db][4 * r4 + 2], O[db][4 * r4 + 3]};
+                *reinterpret_cast<f32x4*>(op + 32 * db + 8 * r4 + 4 * g) = f;
+              }
+            if (g == 0) {
+              const f32x2 ml = {m_run, l_tot};
+              *reinterpret_cast<f32x2*>(a.part_ml + 2 * at) = ml;
+            }
+          }
+          my_row_valid = false;
+        }
+      }
       if (my_row_valid) {
         const float inv = l_tot > 0.0f ? 1.0f / l_tot : 0.0f;
-        uint16_t* op = a.out + b * a.o_sb + h * a.o_sh + (int64_t)row * a.o_sl;
+        uint16_t* op = a.out + b * a.o_sb + (CROSS ? my_head : h) * a.o_sh + (int64_t)(CROSS ? my_pos : row) * a.o_sl;
 #pragma unroll
         for (int db = 0; db < C::DBLK; db++)
 #pragma unroll

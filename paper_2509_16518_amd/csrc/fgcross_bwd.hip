@@ -1,0 +1,497 @@
+// Cross attention, backward.  With P = exp(scale Q K^T - lse) and D_i = sum_d dO_i O_i:
+//   dV = P^T dO,  dP = dO V^T,  dS = P (dP - D),  dQ = scale dS K,  dK = scale dS^T Q.
+// Two kernels, each of which forms S and dP again (14 d flop per score instead of 10): neither needs atomics, so results are the
+// same bits every time.
+//   dq_kernel    a wave owns 32 query rows (Q and dO in registers, one query per lane); the keys stream through LDS.
+//                It also forms D and leaves (lse, D) of every row for the second kernel.
+//   dkdv_kernel  a wave owns 32 keys (K in registers, one key per lane, its V rows in LDS); the queries stream through LDS.  With few
+//                keys and many queries the query rows are split over workgroups, whose fp32 partial sums a third kernel adds up in
+//                a fixed order.
+// Both contractions over a streamed tile read it twice: row-wise (A operand of S or dP) and transposed (A operand of the
+// product that sums over its rows, ds_read_b64_tr_b16).  P and dS are rounded to bf16 as the matrix instructions' operands.
+#include <mutex>
+
+#include "fgattn_fwd.hpp"
+#include "fgcross.hpp"
+
+namespace fgx {
+
+using namespace fg;
+
+struct BwdArgs {
+  const uint16_t *q, *k, *v, *o, *dout;
+  const float* lse;
+  uint16_t *dq, *dk, *dv;
+  const int32_t *q_lens, *k_lens;
+  float* stats;     // [B][H][Lq][2]: lse in log2 units, D
+  float* part;      // dkdv_kernel with several ranges of rows: [n_split][slice][Lk][2][d]
+  int64_t q_sb, q_sh, q_sl, k_sb, k_sh, k_sl, v_sb, v_sh, v_sl, o_sb, o_sh, o_sl;
+  int64_t do_sb, do_sh, do_sl, dq_sb, dq_sh, dq_sl, dk_sb, dk_sh, dk_sl, dv_sb, dv_sh, dv_sl;
+  int32_t B, H, Hkv, group, Lq, Lk;
+  int32_t n_items, QB, KB, n_split, units, units_per_split;   // KB: key tiles of a slice; units: 32-row tiles of a key head's rows
+  float scale, c_log2;
+};
+
+// Tiles of 32 rows of d elements in LDS, 16-byte chunks swizzled so that both reads are free of bank conflicts: chunk c of row r
+// lies at c ^ swz(r).  A row-wise read touches one chunk of 16 consecutive rows at a time, which swz spreads over all 16
+// bank groups; a transposed read touches 64 bytes of 4 consecutive rows, which the upper bits of swz put into 4 of them.
+//   d = 128 (rows of 256 bytes): swz(r) = (r & 3) << 2 | (r >> 2) & 3
+//   d =  64 (rows of 128 bytes, two to a sweep of the banks): swz(r) = (r >> 1 & 1) << 2 | (r >> 2) & 3
+template <int D>
+struct Tile {
+  static constexpr int CH = D / 8, ROWB = D * 2, RPI = 64 / CH, BYTES = 32 * ROWB;
+  static constexpr int SSTEPS = D / 16, DBLK = D / 32;
+  static __device__ __forceinline__ int swz(int r) { return (((D == 128 ? r : r >> 1) & (D == 128 ? 3 : 1)) << 2) | ((r >> 2) & 3); }
+};
+
+// What a lane needs to read a tile: row-wise, lane -> row `ln`, chunk 2 s + g; transposed, 16-lane group (g, u), lane n = 4 kq + qq ->
+// row 4 g + kq (+ 8 for the upper half, + 16 per step c), elements 32 db + 16 u + 4 qq.
+template <int D>
+struct TileReader {
+  using T = Tile<D>;
+  int row_off;
+  int tr_off[T::DBLK];
+  __device__ __forceinline__ void place(int lane) {
+    const int g = lane >> 5, ln = lane & 31, u = (lane >> 4) & 1, kq = (lane & 15) >> 2, qq = lane & 3;
+    row_off = ln * T::ROWB | ((g ^ T::swz(ln)) << 4);
+#pragma unroll
+    for (int db = 0; db < T::DBLK; db++) {
+      const int r = 4 * g + kq;
+      tr_off[db] = r * T::ROWB + (((4 * db + 2 * u + (qq >> 1)) ^ T::swz(r)) << 4) + ((qq & 1) << 3);
+    }
+  }
+  __device__ __forceinline__ bf16x8 rows(const unsigned char* tile, int s) const {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(tile + (row_off ^ (32 * s))));
+  }
+  __device__ __forceinline__ bf16x8 transposed(const unsigned char* tile, int db, int c) const {
+    // (rows 8 further down: bit 1 of the swizzle's lower part flips)
+    const unsigned char* p = tile + 16 * c * T::ROWB;
+    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FG_LDS s16x4*)(p + tr_off[db]));
+    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FG_LDS s16x4*)(p + 8 * T::ROWB + (tr_off[db] ^ 32)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// One 1 KiB load of the wave into LDS (see gather16_first), with a base that may just have been moved to scalar registers by
+// vector instructions: five wait states before the load reads it.
+__device__ __forceinline__ void gather16(const void* base, unsigned byte_off, unsigned lds_base) {
+  base = pin_scalar(base);
+  lds_base = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_base);
+  asm volatile(
+      "s_mov_b32 m0, %2 ; fg_m0\n\t"
+      "s_nop 4\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(byte_off), "s"(base), "s"(lds_base)
+      : "memory", "m0");
+}
+
+// `N_ROWS` rows of a tile (a multiple of RPI, from row r0 of the tile on) from global memory into LDS by LDS-DMA: lane
+// (row, chunk pc) fetches logical chunk pc ^ swz(row).  Rows past `last` are read as row `last`: what is multiplied by an exact
+// zero has to be finite wherever the tensor is.
+template <int D, int N_ROWS>
+__device__ __forceinline__ void fetch_rows(const void* base, unsigned row_bytes, int first, int last, int r0, unsigned lds, int lane) {
+  using T = Tile<D>;
+  const int lrow = lane / T::CH, pc = lane % T::CH;
+#pragma unroll
+  for (int i = 0; i < N_ROWS / T::RPI; i++) {
+    const int r = r0 + i * T::RPI + lrow;
+    const unsigned off = __umul24((unsigned)min(first + r, last), row_bytes) + (unsigned)((pc ^ T::swz(r & 31)) << 4);
+    gather16(base, off, lds + (r0 + i * T::RPI) * T::ROWB);
+  }
+}
+
+__device__ __forceinline__ int xcd_item(int n_items) {   // a contiguous eighth of the items per XCD
+  const int r = blockIdx.x & 7, per = n_items >> 3, rem = n_items & 7;
+  return r * per + min(r, rem) + (blockIdx.x >> 3);
+}
+
+__device__ __forceinline__ void pack_rows(const f32x16& x, bf16x8 (&out)[2]) {   // accumulator -> B operands of two MFMA steps
+#pragma unroll
+  for (int c = 0; c < 2; c++) {
+    f32x8 f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = x[8 * c + e];
+    out[c] = __builtin_convertvector(f, bf16x8);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int g) {
+#pragma unroll
+  for (int db = 0; db < D / 32; db++)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; r4++) {
+      f32x4 f;
+#pragma unroll
+      for (int e = 0; e < 4; e++) f[e] = acc[db][4 * r4 + e] * factor;
+      *reinterpret_cast<i32x2*>(row + 32 * db + 8 * r4 + 4 * g) = __builtin_bit_cast(i32x2, __builtin_convertvector(f, bf16x4));
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) dq_kernel(const BwdArgs a) {
+  using T = Tile<D>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * T::BYTES];   // K and V, two slots each
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w = xcd_item(a.n_items);
+  const int slice = w / a.QB, qi = w - slice * a.QB;
+  const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
+  const int rows = a.group * a.Lq;
+  const int my_row = qi * 128 + wv * 32 + ln;
+  const int row = min(my_row, rows - 1);
+  const int of_group = (int)((unsigned)row / (unsigned)a.Lq), pos = row - of_group * a.Lq;
+  const int head = hk * a.group + of_group;
+  const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
+  const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+  const bool counts = my_row < rows && pos < q_len && k_len > 0;
+
+  bf16x8 qf[T::SSTEPS], dof[T::SSTEPS];
+  float delta = 0.0f;
+  {
+    const char* qp = reinterpret_cast<const char*>(a.q + b * a.q_sb + head * a.q_sh + (int64_t)pos * a.q_sl);
+    const char* op = reinterpret_cast<const char*>(a.o + b * a.o_sb + head * a.o_sh + (int64_t)pos * a.o_sl);
+    const char* dp = reinterpret_cast<const char*>(a.dout + b * a.do_sb + head * a.do_sh + (int64_t)pos * a.do_sl);
+#pragma unroll
+    for (int s = 0; s < T::SSTEPS; s++) {
+      i32x4 zero = {0, 0, 0, 0}, qr = zero, dr = zero, orow = zero;
+      if (counts) {   // (rows that do not count may hold anything)
+        qr = *reinterpret_cast<const i32x4*>(qp + (2 * s + g) * 16);
+        dr = *reinterpret_cast<const i32x4*>(dp + (2 * s + g) * 16);
+        orow = *reinterpret_cast<const i32x4*>(op + (2 * s + g) * 16);
+      }
+      qf[s] = __builtin_bit_cast(bf16x8, qr);
+      dof[s] = __builtin_bit_cast(bf16x8, dr);
+      const bf16x8 of = __builtin_bit_cast(bf16x8, orow);
+#pragma unroll
+      for (int e = 0; e < 8; e++) delta += (float)of[e] * (float)dof[s][e];
+    }
+  }
+  delta = lane_pair_sum(delta);
+  const int64_t at = ((int64_t)b * a.H + head) * a.Lq + pos;
+  const float lse2 = counts ? a.lse[at] * 1.44269504088896340736f : INFINITY;
+  if (counts && g == 0) {
+    const f32x2 st = {lse2, delta};
+    *reinterpret_cast<f32x2*>(a.stats + 2 * at) = st;
+  }
+
+  f32x16 acc[T::DBLK];
+#pragma unroll
+  for (int db = 0; db < T::DBLK; db++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) acc[db][r] = 0.0f;
+  const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh;
+  const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh;
+  const unsigned k_rowb = (unsigned)(a.k_sl * 2), v_rowb = (unsigned)(a.v_sl * 2);
+  const unsigned lds0 = lds_address(smem);
+  TileReader<D> rd;
+  rd.place(lane);
+  const int ntiles = (k_len + 31) / 32;
+  auto fetch = [&](int t) {
+    const unsigned slot = lds0 + (t & 1) * 2 * T::BYTES;
+    fetch_rows<D, 8>(kbase, k_rowb, t * 32, k_len - 1, wv * 8, slot, lane);
+    fetch_rows<D, 8>(vbase, v_rowb, t * 32, k_len - 1, wv * 8, slot + T::BYTES, lane);
+  };
+  if (ntiles > 0) fetch(0);
+  for (int t = 0; t < ntiles; t++) {
+    wait_vmem_all();
+    __syncthreads();   // tile t is there, and every wave is done with the slot of tile t + 1
+    if (t + 1 < ntiles) fetch(t + 1);
+    const unsigned char* kt = smem + (t & 1) * 2 * T::BYTES;
+    const unsigned char* vt = kt + T::BYTES;
+    f32x16 S, dP;
+#pragma unroll
+    for (int r = 0; r < 16; r++) S[r] = dP[r] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < T::SSTEPS; s++) {
+      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.rows(kt, s), qf[s], S, 0, 0, 0);
+      dP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.rows(vt, s), dof[s], dP, 0, 0, 0);
+    }
+    f32x16 dS;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], a.c_log2, -lse2));
+      dS[r] = p * (dP[r] - delta);
+    }
+    if (t * 32 + 32 > k_len) {
+#pragma unroll
+      for (int r = 0; r < 16; r++)
+        if (t * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= k_len) dS[r] = 0.0f;
+    }
+    bf16x8 ds[2];
+    pack_rows(dS, ds);
+#pragma unroll
+    for (int db = 0; db < T::DBLK; db++)
+#pragma unroll
+      for (int c = 0; c < 2; c++)
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.transposed(kt, db, c), ds[c], acc[db], 0, 0, 0);
+  }
+  if (my_row < rows)   // (zeros where the row does not count)
+    store_row<D>(a.dq + b * a.dq_sb + head * a.dq_sh + (int64_t)pos * a.dq_sl, acc, counts ? a.scale : 0.0f, g);
+}
+
+template <int D>
+constexpr int dkdv_lds_bytes() {
+  return 4 * Tile<D>::BYTES + 4 * Tile<D>::BYTES + 2 * 32 * 2 * (int)sizeof(float);   // Q and dO, two slots each; V of 128 keys; (lse, D), two slots
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) dkdv_kernel(const BwdArgs a) {
+  using T = Tile<D>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w = xcd_item(a.n_items);
+  const int kb = w % a.KB, split = w / a.KB % a.n_split, slice = w / a.KB / a.n_split;
+  const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
+  const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
+  const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+  const int key0 = kb * 128, my_key = key0 + wv * 32 + ln;
+  const bool any = key0 < k_len && q_len > 0;
+  if (!any && a.n_split > 1) return;   // (the kernel that adds up the ranges knows)
+
+  f32x16 dk[T::DBLK], dv[T::DBLK];
+#pragma unroll
+  for (int db = 0; db < T::DBLK; db++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) dk[db][r] = dv[db][r] = 0.0f;
+
+  if (any) {
+    const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh;
+    const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh;
+    const unsigned lds0 = lds_address(smem);
+    unsigned char* const vt = smem + 4 * T::BYTES + wv * T::BYTES;   // this wave's 32 rows of V
+    float* const stats = reinterpret_cast<float*>(smem + 8 * T::BYTES);
+    bf16x8 kf[T::SSTEPS];
+    {
+      const char* kp = reinterpret_cast<const char*>(kbase + (int64_t)min(my_key, k_len - 1) * a.k_sl);
+#pragma unroll
+      for (int s = 0; s < T::SSTEPS; s++) kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(kp + (2 * s + g) * 16));
+    }
+    fetch_rows<D, 32>(vbase, (unsigned)(a.v_sl * 2), key0 + wv * 32, k_len - 1, 0, lds0 + 4 * T::BYTES + wv * T::BYTES, lane);
+    TileReader<D> rd;
+    rd.place(lane);
+    const unsigned q_rowb = (unsigned)(a.q_sl * 2), do_rowb = (unsigned)(a.do_sl * 2);
+    // unit u of the slice = 32-row tile u % (tiles of a head) of head u / (tiles of a head) of the group
+    const int per_head = (a.Lq + 31) / 32;
+    const int u0 = split * a.units_per_split, u1 = min(u0 + a.units_per_split, a.units);
+    int hl = u0 / per_head, tile = u0 - hl * per_head;   // of the unit that is fetched next
+    float st = 0.0f;                                     // the value of (lse, D) that this lane fetches
+    auto fetch = [&](int slot) {
+      const int head = hk * a.group + hl;
+      const unsigned lds = lds0 + slot * 2 * T::BYTES;
+      const int first = tile * 32;
+      fetch_rows<D, 8>(a.q + b * a.q_sb + head * a.q_sh, q_rowb, first, q_len - 1, wv * 8, lds, lane);
+      fetch_rows<D, 8>(a.dout + b * a.do_sb + head * a.do_sh, do_rowb, first, q_len - 1, wv * 8, lds + T::BYTES, lane);
+      if (tid < 64) {   // rows past the end: lse = +inf, so that P = 0, and D = 0
+        const int r = first + (tid >> 1);
+        st = r < q_len ? a.stats[2 * (((int64_t)b * a.H + head) * a.Lq + r) + (tid & 1)] : (tid & 1) ? 0.0f : INFINITY;
+      }
+      if (++tile == per_head) {
+        tile = 0;
+        hl++;
+      }
+    };
+    // (a unit behind the last token of a shorter sequence is fetched as copies of its last row, with P = 0)
+    if (u0 < u1) {
+      fetch(0);
+      if (tid < 64) stats[tid] = st;
+    }
+    for (int u = u0; u < u1; u++) {
+      const int slot = (u - u0) & 1;
+      wait_vmem_all();
+      __syncthreads();
+      if (u + 1 < u1) fetch(slot ^ 1);
+      const unsigned char* qt = smem + slot * 2 * T::BYTES;
+      const unsigned char* dot = qt + T::BYTES;
+      const float* stt = stats + slot * 64;
+      f32x16 S, dP;
+#pragma unroll
+      for (int r = 0; r < 16; r++) S[r] = dP[r] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < T::SSTEPS; s++) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.rows(qt, s), kf[s], S, 0, 0, 0);
+#pragma unroll
+      for (int s = 0; s < T::SSTEPS; s++) dP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.rows(dot, s), rd.rows(vt, s), dP, 0, 0, 0);
+      f32x16 dS;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; r4++) {
+        const f32x4 s0 = *reinterpret_cast<const f32x4*>(stt + 2 * (8 * r4 + 4 * g));
+        const f32x4 s1 = *reinterpret_cast<const f32x4*>(stt + 2 * (8 * r4 + 4 * g) + 4);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float lse2 = e < 2 ? s0[2 * e] : s1[2 * e - 4], delta = e < 2 ? s0[2 * e + 1] : s1[2 * e - 3];
+          const int r = 4 * r4 + e;
+          S[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], a.c_log2, -lse2));
+          dS[r] = S[r] * (dP[r] - delta);
+        }
+      }
+      bf16x8 p[2], ds[2];
+      pack_rows(S, p);
+      pack_rows(dS, ds);
+#pragma unroll
+      for (int db = 0; db < T::DBLK; db++)
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+          dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.transposed(dot, db, c), p[c], dv[db], 0, 0, 0);
+          dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.transposed(qt, db, c), ds[c], dk[db], 0, 0, 0);
+        }
+      if (u + 1 < u1 && tid < 64) stats[(slot ^ 1) * 64 + tid] = st;
+    }
+  }
+  if (a.n_split > 1) {
+    if (my_key < k_len) {
+      float* row = a.part + ((((int64_t)split * a.B * a.Hkv + slice) * a.Lk + my_key) * 2) * D;
+#pragma unroll
+      for (int db = 0; db < T::DBLK; db++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) {
+          const int e = 32 * db + 8 * r4 + 4 * g;
+          *reinterpret_cast<f32x4*>(row + e) = f32x4{dk[db][4 * r4], dk[db][4 * r4 + 1], dk[db][4 * r4 + 2], dk[db][4 * r4 + 3]};
+          *reinterpret_cast<f32x4*>(row + D + e) = f32x4{dv[db][4 * r4], dv[db][4 * r4 + 1], dv[db][4 * r4 + 2], dv[db][4 * r4 + 3]};
+        }
+    }
+  } else if (my_key < a.Lk) {
+    const bool counts = my_key < k_len;
+    store_row<D>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)my_key * a.dk_sl, dk, counts ? a.scale : 0.0f, g);
+    store_row<D>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)my_key * a.dv_sl, dv, counts ? 1.0f : 0.0f, g);
+  }
+}
+
+// dK and dV of split rows: a thread adds up four elements of one key over the ranges, in order.
+template <int D>
+__global__ void __launch_bounds__(256) sum_kernel(const BwdArgs a) {
+  constexpr int PER = 2 * D / 4;   // threads of a key
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = t / PER;
+  const int e = (int)(t - row * PER) * 4;
+  const int64_t n_rows = (int64_t)a.B * a.Hkv * a.Lk;
+  if (row >= n_rows) return;
+  const int slice = (int)(row / a.Lk), key = (int)(row - (int64_t)slice * a.Lk);
+  const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
+  const int q_len = a.q_lens ? min(a.q_lens[b], a.Lq) : a.Lq, k_len = a.k_lens ? a.k_lens[b] : a.Lk;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (key < k_len && q_len > 0) {
+    const float* src = a.part + row * 2 * D + e;
+    for (int s = 0; s < a.n_split; s++) sum += *reinterpret_cast<const f32x4*>(src + s * n_rows * 2 * D);
+  }
+  uint16_t* dst;
+  if (e < D) {
+    sum *= a.scale;
+    dst = a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)key * a.dk_sl + e;
+  } else {
+    dst = a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)key * a.dv_sl + e - D;
+  }
+  *reinterpret_cast<i32x2*>(dst) = __builtin_bit_cast(i32x2, __builtin_convertvector(sum, bf16x4));
+}
+
+struct BwdPlan {
+  int QB, KB, units, n_split, units_per_split;
+  size_t stats_bytes, bytes;
+};
+static BwdPlan bwd_plan(const fgattn_cross_params* p) {
+  BwdPlan s;
+  const int64_t slices = (int64_t)p->B * p->Hkv;
+  const int group = p->H / p->Hkv;
+  s.QB = (int)(((int64_t)group * p->Lq + 127) / 128);
+  s.KB = (p->Lk + 127) / 128;
+  s.units = group * ((p->Lq + 31) / 32);
+  const int64_t tiles = slices * s.KB;
+  int64_t n = tiles < 512 ? 512 / tiles : 1;
+  if (n > s.units) n = s.units;
+  s.units_per_split = (int)((s.units + n - 1) / n);
+  s.n_split = (s.units + s.units_per_split - 1) / s.units_per_split;
+  s.stats_bytes = ((size_t)p->B * p->H * p->Lq * 2 * sizeof(float) + 255) & ~(size_t)255;
+  s.bytes = s.stats_bytes;
+  if (s.n_split > 1) s.bytes += ((size_t)s.n_split * slices * p->Lk * 2 * p->d * sizeof(float) + 255) & ~(size_t)255;
+  return s;
+}
+
+template <int D>
+static int launch_bwd(BwdArgs& a, const BwdPlan& s, hipStream_t stream) {
+  static std::mutex mutex;
+  static bool ready[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return FGATTN_E_DEVICE;
+  {
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!ready[dev]) {
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(dkdv_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                              dkdv_lds_bytes<D>()) != hipSuccess)
+        return FGATTN_E_DEVICE;
+      ready[dev] = true;
+    }
+  }
+  const int slices = a.B * a.Hkv;
+  a.n_items = slices * s.QB;
+  hipLaunchKernelGGL(dq_kernel<D>, dim3(a.n_items), dim3(256), 0, stream, a);
+  if (hipGetLastError() != hipSuccess) return FGATTN_E_DEVICE;
+  a.n_items = slices * s.KB * s.n_split;
+  hipLaunchKernelGGL(dkdv_kernel<D>, dim3(a.n_items), dim3(256), dkdv_lds_bytes<D>(), stream, a);
+  if (hipGetLastError() != hipSuccess) return FGATTN_E_DEVICE;
+  if (s.n_split > 1) {
+    const int64_t threads = (int64_t)slices * a.Lk * (2 * D / 4);
+    hipLaunchKernelGGL(sum_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
+    if (hipGetLastError() != hipSuccess) return FGATTN_E_DEVICE;
+  }
+  return FGATTN_OK;
+}
+
+}  // namespace fgx
+
+extern "C" {
+
+size_t fgattn_cross_backward_workspace_bytes(const fgattn_cross_params* p) {
+  return fgx::check_shape(p) == FGATTN_OK ? fgx::bwd_plan(p).bytes : 0;
+}
+
+int fgattn_cross_backward(const void* q, const void* k, const void* v, const void* out, const float* lse, const void* dout,
+                          const int32_t* q_lens, const int32_t* k_lens, const fgattn_cross_params* p, void* dq, void* dk,
+                          void* dv, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = fgx::check_shape(p);
+  if (rc) return rc;
+  if (!lse) return FGATTN_E_NULL;
+  if ((rc = fgx::check_tensor(q, p->q_stride_b, p->q_stride_h, p->q_stride_l, p->B, p->H, p->Lq, p->d, true, false))) return rc;
+  if ((rc = fgx::check_tensor(k, p->k_stride_b, p->k_stride_h, p->k_stride_l, p->B, p->Hkv, p->Lk, p->d, true, false))) return rc;
+  if ((rc = fgx::check_tensor(v, p->v_stride_b, p->v_stride_h, p->v_stride_l, p->B, p->Hkv, p->Lk, p->d, true, false))) return rc;
+  if ((rc = fgx::check_tensor(out, p->o_stride_b, p->o_stride_h, p->o_stride_l, p->B, p->H, p->Lq, p->d, false, false))) return rc;
+  if ((rc = fgx::check_tensor(dout, p->do_stride_b, p->do_stride_h, p->do_stride_l, p->B, p->H, p->Lq, p->d, true, false))) return rc;
+  if ((rc = fgx::check_tensor(dq, p->dq_stride_b, p->dq_stride_h, p->dq_stride_l, p->B, p->H, p->Lq, p->d, false, true))) return rc;
+  if ((rc = fgx::check_tensor(dk, p->dk_stride_b, p->dk_stride_h, p->dk_stride_l, p->B, p->Hkv, p->Lk, p->d, false, true))) return rc;
+  if ((rc = fgx::check_tensor(dv, p->dv_stride_b, p->dv_stride_h, p->dv_stride_l, p->B, p->Hkv, p->Lk, p->d, false, true))) return rc;
+  if ((reinterpret_cast<uintptr_t>(lse) & 3) != 0) return FGATTN_E_ALIGN;
+  if ((rc = fgx::check_lens(q_lens, k_lens))) return rc;
+  const fgx::BwdPlan s = fgx::bwd_plan(p);
+  if ((rc = fgx::check_workspace(workspace, workspace_bytes, s.bytes))) return rc;
+  if ((rc = fg::require_device(nullptr))) return rc;
+  fgx::BwdArgs a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.o = static_cast<const uint16_t*>(out);
+  a.dout = static_cast<const uint16_t*>(dout);
+  a.lse = lse;
+  a.dq = static_cast<uint16_t*>(dq);
+  a.dk = static_cast<uint16_t*>(dk);
+  a.dv = static_cast<uint16_t*>(dv);
+  a.q_lens = q_lens;
+  a.k_lens = k_lens;
+  a.stats = static_cast<float*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + s.stats_bytes);
+  a.q_sb = p->q_stride_b; a.q_sh = p->q_stride_h; a.q_sl = p->q_stride_l;
+  a.k_sb = p->k_stride_b; a.k_sh = p->k_stride_h; a.k_sl = p->k_stride_l;
+  a.v_sb = p->v_stride_b; a.v_sh = p->v_stride_h; a.v_sl = p->v_stride_l;
+  a.o_sb = p->o_stride_b; a.o_sh = p->o_stride_h; a.o_sl = p->o_stride_l;
+  a.do_sb = p->do_stride_b; a.do_sh = p->do_stride_h; a.do_sl = p->do_stride_l;
+  a.dq_sb = p->dq_stride_b; a.dq_sh = p->dq_stride_h; a.dq_sl = p->dq_stride_l;
+  a.dk_sb = p->dk_stride_b; a.dk_sh = p->dk_stride_h; a.dk_sl = p->dk_stride_l;
+  a.dv_sb = p->dv_stride_b; a.dv_sh = p->dv_stride_h; a.dv_sl = p->dv_stride_l;
+  a.B = p->B; a.H = p->H; a.Hkv = p->Hkv; a.group = p->H / p->Hkv; a.Lq = p->Lq; a.Lk = p->Lk;
+  a.QB = s.QB; a.KB = s.KB; a.n_split = s.n_split; a.units = s.units; a.units_per_split = s.units_per_split;
+  a.scale = p->scale;
+  a.c_log2 = p->scale * 1.44269504088896340736f;
+  return p->d == 64 ? fgx::launch_bwd<64>(a, s, static_cast<hipStream_t>(stream))
+                    : fgx::launch_bwd<128>(a, s, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

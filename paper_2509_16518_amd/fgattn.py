@@ -20,9 +20,31 @@ class FgattnParams(ctypes.Structure):
                 ("scale", ctypes.c_float), ("flags", ctypes.c_int32)]
 
 
+class FgattnRopeAxis(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("pairs", ctypes.c_int32), ("theta", ctypes.c_double), ("offset", ctypes.c_double),
+                ("step", ctypes.c_double), ("factor", ctypes.c_double), ("original", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
+
+
+class FgattnRopeParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("rot_dims", ctypes.c_int32), ("layout", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32),
+                ("eps", ctypes.c_float)] + [("%s_stride_%s" % (t, x), ctypes.c_int64) for t in ("q", "k", "qo", "ko") for x in "bhl"]
+
+
+class FgattnCrossParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Lq", ctypes.c_int32), ("Lk", ctypes.c_int32),
+                ("d", ctypes.c_int32)] + \
+        [("%s_stride_%s" % (t, x), ctypes.c_int64) for t in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for x in "bhl"] + \
+        [("scale", ctypes.c_float), ("flags", ctypes.c_int32)]
+
+
 FLAG_STATIC_ASSIGN, FLAG_FIFO_QUEUE, FLAG_REUSE_PLAN, FLAG_MASK_ROWS_IN_HBM, FLAG_MASK_ONE_TILE_CHUNKS = 1, 2, 4, 8, 16
-E_NULL, E_SHAPE, E_STRIDE, E_ALIGN, E_WORKSPACE, E_SCALE, E_DEVICE, E_MASK, E_FLAGS, E_STATIC_LIMIT = range(-1, -11, -1)
+E_NULL, E_SHAPE, E_STRIDE, E_ALIGN, E_WORKSPACE, E_SCALE, E_DEVICE, E_MASK, E_FLAGS, E_STATIC_LIMIT, E_DTYPE = range(-1, -12, -1)
 STATIC_MAX_ITEMS = 65536
+BF16, FP16, FP32 = 0, 1, 2
+ROPE_INTERLEAVED, ROPE_HALF = 0, 1
+FLAG_ROPE_NORM, FLAG_ROPE_WEIGHT_FP32 = 1, 2
 
 _lib = None
 
@@ -72,6 +94,23 @@ def lib():
         L.fgattn_group_select.restype = ctypes.c_int
         L.fgattn_group_emit.argtypes = [pp, ctypes.c_int, vp, vp, vp, vp, ctypes.c_int64, vp, ctypes.c_size_t, vp]
         L.fgattn_group_emit.restype = ctypes.c_int
+        rp, xp, sz = ctypes.POINTER(FgattnRopeParams), ctypes.POINTER(FgattnCrossParams), ctypes.c_size_t
+        L.fgattn_rope_table.argtypes = [ctypes.POINTER(FgattnRopeAxis), ctypes.c_int, ctypes.c_float, vp, vp, vp]
+        L.fgattn_rope_table.restype = ctypes.c_int
+        L.fgattn_rope_forward.argtypes = [vp] * 6 + [ctypes.c_int32, vp, rp, vp, vp, vp]
+        L.fgattn_rope_forward.restype = ctypes.c_int
+        L.fgattn_rope_workspace_bytes.argtypes = [rp]
+        L.fgattn_rope_workspace_bytes.restype = sz
+        L.fgattn_rope_backward.argtypes = [vp] * 6 + [ctypes.c_int32, vp, rp] + [vp] * 7 + [sz, vp]
+        L.fgattn_rope_backward.restype = ctypes.c_int
+        L.fgattn_cross_workspace_bytes.argtypes = [xp]
+        L.fgattn_cross_workspace_bytes.restype = sz
+        L.fgattn_cross_forward.argtypes = [vp] * 5 + [xp, vp, vp, vp, sz, vp]
+        L.fgattn_cross_forward.restype = ctypes.c_int
+        L.fgattn_cross_backward_workspace_bytes.argtypes = [xp]
+        L.fgattn_cross_backward_workspace_bytes.restype = sz
+        L.fgattn_cross_backward.argtypes = [vp] * 8 + [xp] + [vp] * 4 + [sz, vp]
+        L.fgattn_cross_backward.restype = ctypes.c_int
         L.fgattn_grid_size.argtypes = [pp]
         L.fgattn_grid_size.restype = ctypes.c_int
         L.fgattn_strerror.argtypes = [ctypes.c_int]
@@ -216,3 +255,202 @@ def fgattn_validate_mask(mask_indptr, mask_indices, params, workspace, stream=No
 
 def fgattn_grid_size(params):
     return int(lib().fgattn_grid_size(ctypes.byref(params)))
+
+
+# ---- rotary positions, norms of queries and keys, cross attention ----
+# These bindings also compare every tensor with the params (the C ABI sees pointers only) and run on the tensors' own device,
+# whichever is current.
+
+def _refuse(code):
+    raise FgattnError(code)
+
+
+def _pointer(t, device, dtype, shape=None, strides=None):
+    """Address of a tensor (None: NULL) on `device`, of `dtype` and, if given, of this shape (contiguous) or these strides."""
+    if t is None:
+        return None
+    if t.device != device:
+        _refuse(E_DEVICE)
+    if t.dtype is not dtype:
+        _refuse(E_DTYPE)
+    if shape is not None and (t.shape != shape or (strides is None and not t.is_contiguous())):
+        _refuse(E_SHAPE)
+    if strides is not None and t.stride() != strides and any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), strides)):
+        _refuse(E_STRIDE)
+    return t.data_ptr()
+
+
+def _launch(device, stream, tensors, call):
+    """call(stream pointer) with `device` current; a stream of another device is refused, and the allocator learns of tensors
+    that are used on a stream other than the current one."""
+    import torch
+    if device.type != "cuda":
+        _refuse(E_DEVICE)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _launch(device, stream, tensors, call)
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    else:
+        if stream.device != device:
+            _refuse(E_DEVICE)
+        if stream != torch.cuda.current_stream():
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+    _check(call(ctypes.c_void_p(stream.cuda_stream)))
+
+
+def fgattn_rope_table(axes, cos, sin, mscale=1.0, stream=None):
+    """Fills cos and sin (fp32 [rows, pairs]) with the angles of a token grid.  axes: one to three tuples (size, pairs, theta,
+    offset, step, factor, original, beta_fast, beta_slow), later ones optional from `offset` on (0, 1, 1, 0, 32, 1)."""
+    import torch
+    n = len(axes)
+    if not 1 <= n <= 3:
+        _refuse(E_SHAPE)
+    table = (FgattnRopeAxis * n)(*[FgattnRopeAxis(*x, *(0.0, 1.0, 1.0, 0.0, 32.0, 1.0)[len(x) - 3:]) for x in axes])
+    rows, pairs = 1, 0
+    for x in table:
+        rows, pairs = rows * x.size, pairs + x.pairs
+    c, s = (_pointer(t, cos.device, torch.float32, (rows, pairs)) for t in (cos, sin))
+    _launch(cos.device, stream, (cos, sin), lambda st: lib().fgattn_rope_table(table, n, mscale, c, s, st))
+
+
+def _dtype_code(dtype):
+    import torch
+    code = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}.get(dtype)
+    return _refuse(E_DTYPE) if code is None else code
+
+
+def make_rope_params(q, k, q_out, k_out, rot_dims, layout=ROPE_INTERLEAVED, eps=1e-6, flags=FLAG_ROPE_NORM):
+    """fgattn_rope_params for [B, H, L, d] tensors (any strides with a contiguous last dim); k and k_out may be None.  For the
+    backward call q_out and k_out are the gradients that come in, and dq and dk have the strides of q and k."""
+    B, Hq, L, d = q.shape
+    for t in (q, k, q_out, k_out):
+        if t is not None and (t.dim() != 4 or t.stride(3) != 1):
+            _refuse(E_STRIDE)
+    if q_out.shape != q.shape or (k is None) != (k_out is None) or \
+            (k is not None and (k.shape != k_out.shape or (k.shape[0], k.shape[2], k.shape[3]) != (B, L, d))):
+        _refuse(E_SHAPE)
+    none = (0, 0, 0)
+    return FgattnRopeParams(B, Hq, 0 if k is None else k.shape[1], L, d, rot_dims, layout, _dtype_code(q.dtype), flags, eps,
+                            *q.stride()[:3], *(none if k is None else k.stride()[:3]), *q_out.stride()[:3],
+                            *(none if k is None else k_out.stride()[:3]))
+
+
+def fgattn_rope_workspace_bytes(params):
+    return int(lib().fgattn_rope_workspace_bytes(ctypes.byref(params)))
+
+
+def _rope_pointers(p, q, k, cos, sin, positions, q_weight, k_weight, device, dtype):
+    import torch
+    if _dtype_code(dtype) != p.dtype:
+        _refuse(E_DTYPE)
+    f32 = torch.float32
+    if (cos is None) != (sin is None):
+        _refuse(E_NULL)
+    w_type = f32 if p.flags & FLAG_ROPE_WEIGHT_FP32 else dtype
+    rows = 0 if cos is None else cos.shape[0]
+    table = (rows, p.rot_dims // 2)
+    return [_pointer(q, device, dtype, (p.B, p.Hq, p.L, p.d), (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
+            _pointer(k, device, dtype, (p.B, p.Hk, p.L, p.d), (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
+            _pointer(q_weight, device, w_type, (p.d,)), _pointer(k_weight, device, w_type, (p.d,)),
+            _pointer(cos, device, f32, table), _pointer(sin, device, f32, table), rows,
+            _pointer(positions, device, torch.int32, (p.B, p.L)), ctypes.byref(p)]
+
+
+def fgattn_rope_forward(q, k, params, q_out, k_out, cos=None, sin=None, positions=None, q_weight=None, k_weight=None, stream=None):
+    """Queries and keys normed per head and turned by their positions (see include/fgattn.h)."""
+    p, dev, dt = params, q.device, q.dtype
+    args = _rope_pointers(p, q, k, cos, sin, positions, q_weight, k_weight, dev, dt)
+    args += [_pointer(q_out, dev, dt, (p.B, p.Hq, p.L, p.d), (p.qo_stride_b, p.qo_stride_h, p.qo_stride_l, 1)),
+             _pointer(k_out, dev, dt, (p.B, p.Hk, p.L, p.d), (p.ko_stride_b, p.ko_stride_h, p.ko_stride_l, 1))]
+    _launch(dev, stream, (q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight),
+            lambda st: lib().fgattn_rope_forward(*args, st))
+
+
+def fgattn_rope_backward(q, k, params, dq_out, dk_out, dq, dk, cos=None, sin=None, positions=None, q_weight=None, k_weight=None,
+                         dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """Gradients of fgattn_rope_forward: dq, dk and, where given, dq_weight and dk_weight (fp32).  q and k may be None without
+    FLAG_ROPE_NORM."""
+    import torch
+    p, dev, dt = params, dq_out.device, dq_out.dtype
+    args = _rope_pointers(p, q, k, cos, sin, positions, q_weight, k_weight, dev, dt)
+    shape_q, shape_k = (p.B, p.Hq, p.L, p.d), (p.B, p.Hk, p.L, p.d)
+    args += [_pointer(dq_out, dev, dt, shape_q, (p.qo_stride_b, p.qo_stride_h, p.qo_stride_l, 1)),
+             _pointer(dk_out, dev, dt, shape_k, (p.ko_stride_b, p.ko_stride_h, p.ko_stride_l, 1)),
+             _pointer(dq, dev, dt, shape_q, (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
+             _pointer(dk, dev, dt, shape_k, (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
+             _pointer(dq_weight, dev, torch.float32, (p.d,)), _pointer(dk_weight, dev, torch.float32, (p.d,)),
+             *_workspace(workspace, dev)]
+    _launch(dev, stream, (q, k, dq_out, dk_out, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, workspace),
+            lambda st: lib().fgattn_rope_backward(*args, st))
+
+
+def _workspace(workspace, device):
+    if workspace is None:
+        return None, 0
+    if workspace.device != device:
+        _refuse(E_DEVICE)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def make_cross_params(q, k, v, out, scale, dout=None, dq=None, dk=None, dv=None):
+    """fgattn_cross_params for q, out [B, H, Lq, d] and k, v [B, Hkv, Lk, d] (any strides with a contiguous last dim); for the
+    backward call also the incoming gradient and the three gradients."""
+    B, H, Lq, d = q.shape
+    Hkv, Lk = k.shape[1], k.shape[2]
+    strides = []
+    for t, shape in ((q, q.shape), (k, (B, Hkv, Lk, d)), (v, (B, Hkv, Lk, d)), (out, q.shape), (dout, q.shape), (dq, q.shape),
+                     (dk, (B, Hkv, Lk, d)), (dv, (B, Hkv, Lk, d))):
+        if t is None:
+            strides += (0, 0, 0)
+            continue
+        if t.shape != shape:
+            _refuse(E_SHAPE)
+        s = t.stride()
+        if len(s) != 4 or s[3] != 1:
+            _refuse(E_STRIDE)
+        strides += s[:3]
+    return FgattnCrossParams(B, H, Hkv, Lq, Lk, d, *strides, scale, 0)
+
+
+def fgattn_cross_workspace_bytes(params):
+    return int(lib().fgattn_cross_workspace_bytes(ctypes.byref(params)))
+
+
+def fgattn_cross_backward_workspace_bytes(params):
+    return int(lib().fgattn_cross_backward_workspace_bytes(ctypes.byref(params)))
+
+
+def fgattn_cross_forward(q, k, v, params, out, lse, workspace=None, q_lens=None, k_lens=None, stream=None):
+    """Attention of q's tokens to k and v, another sequence with its own lengths (see include/fgattn.h)."""
+    import torch
+    p, dev, bf16 = params, q.device, torch.bfloat16
+    shape_q, shape_k = (p.B, p.H, p.Lq, p.d), (p.B, p.Hkv, p.Lk, p.d)
+    args = [_pointer(q, dev, bf16, shape_q, (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
+            _pointer(k, dev, bf16, shape_k, (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
+            _pointer(v, dev, bf16, shape_k, (p.v_stride_b, p.v_stride_h, p.v_stride_l, 1)),
+            _pointer(q_lens, dev, torch.int32, (p.B,)), _pointer(k_lens, dev, torch.int32, (p.B,)), ctypes.byref(p),
+            _pointer(out, dev, bf16, shape_q, (p.o_stride_b, p.o_stride_h, p.o_stride_l, 1)),
+            _pointer(lse, dev, torch.float32, shape_q[:3]), *_workspace(workspace, dev)]
+    _launch(dev, stream, (q, k, v, out, lse, workspace, q_lens, k_lens), lambda st: lib().fgattn_cross_forward(*args, st))
+
+
+def fgattn_cross_backward(q, k, v, out, lse, dout, params, dq, dk, dv, workspace, q_lens=None, k_lens=None, stream=None):
+    """Gradients of fgattn_cross_forward with respect to q, k and v, from its inputs and results and the gradient of out."""
+    import torch
+    p, dev, bf16 = params, q.device, torch.bfloat16
+    shape_q, shape_k = (p.B, p.H, p.Lq, p.d), (p.B, p.Hkv, p.Lk, p.d)
+    args = [_pointer(q, dev, bf16, shape_q, (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
+            _pointer(k, dev, bf16, shape_k, (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
+            _pointer(v, dev, bf16, shape_k, (p.v_stride_b, p.v_stride_h, p.v_stride_l, 1)),
+            _pointer(out, dev, bf16, shape_q, (p.o_stride_b, p.o_stride_h, p.o_stride_l, 1)),
+            _pointer(lse, dev, torch.float32, shape_q[:3]),
+            _pointer(dout, dev, bf16, shape_q, (p.do_stride_b, p.do_stride_h, p.do_stride_l, 1)),
+            _pointer(q_lens, dev, torch.int32, (p.B,)), _pointer(k_lens, dev, torch.int32, (p.B,)), ctypes.byref(p),
+            _pointer(dq, dev, bf16, shape_q, (p.dq_stride_b, p.dq_stride_h, p.dq_stride_l, 1)),
+            _pointer(dk, dev, bf16, shape_k, (p.dk_stride_b, p.dk_stride_h, p.dk_stride_l, 1)),
+            _pointer(dv, dev, bf16, shape_k, (p.dv_stride_b, p.dv_stride_h, p.dv_stride_l, 1)), *_workspace(workspace, dev)]
+    _launch(dev, stream, (q, k, v, out, lse, dout, dq, dk, dv, workspace, q_lens, k_lens),
+            lambda st: lib().fgattn_cross_backward(*args, st))
