@@ -11,7 +11,7 @@
 // product that sums over its rows, ds_read_b64_tr_b16).  P and dS are rounded to bf16 as the matrix instructions' operands.
 #include <mutex>
 
-#include "fgattn_fwd.hpp"
+#include "fgcross_fwd.hpp"
 #include "fgcross.hpp"
 
 namespace fgx {
@@ -71,20 +71,6 @@ struct TileReader {
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
-
-// One 1 KiB load of the wave into LDS (see gather16_first), with a base that may just have been moved to scalar registers by
-// vector instructions: five wait states before the load reads it.
-__device__ __forceinline__ void gather16(const void* base, unsigned byte_off, unsigned lds_base) {
-  base = pin_scalar(base);
-  lds_base = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_base);
-  asm volatile(
-      "s_mov_b32 m0, %2 ; fg_m0\n\t"
-      "s_nop 4\n\t"
-      "global_load_lds_dwordx4 %0, %1"
-      :
-      : "v"(byte_off), "s"(base), "s"(lds_base)
-      : "memory", "m0");
-}
 
 // `N_ROWS` rows of a tile (a multiple of RPI, from row r0 of the tile on) from global memory into LDS by LDS-DMA: lane
 // (row, chunk pc) fetches logical chunk pc ^ swz(row).  Rows past `last` are read as row `last`: what is multiplied by an exact

@@ -6,9 +6,12 @@
 // matrix pipe.  Calls with few rows run 32-row tiles in single-wave workgroups, each against a range of the keys; their
 // bound is reading K and V once, which takes as many waves in flight as LDS holds.  A second kernel joins the
 // ranges: with m_s, l_s, O_s of range s, out = sum O_s e^(m_s - m) / sum l_s e^(m_s - m).
+#include <mutex>
+
 #include "fgattn_fwd.hpp"
 #include "fgattn_launch.hpp"
 #include "fgcross.hpp"
+#include "fgcross_fwd.hpp"
 
 namespace fgx {
 
@@ -65,7 +68,12 @@ __global__ void __launch_bounds__(256) join_kernel(const JoinArgs a) {
   if (lane == 0) a.lse[at] = total > 0.0f ? a.scale_abs * top + __logf(total) : -INFINITY;
 }
 
+// LDS of a key head's tiles (K and V, 32 keys each) and how many tiles a workgroup can hold.
+constexpr int kLds = 160 * 1024;
+static int resident_bytes(const fgattn_cross_params* p) { return (p->Lk + 63) / 64 * 64 * 4 * p->d; }
+
 struct Plan {
+  bool resident;
   int M, QB, n_split, split_keys;
   int64_t items;
 };
@@ -74,10 +82,12 @@ static Plan plan_of(const fgattn_cross_params* p) {
   const int rows = p->H / p->Hkv * p->Lq;
   const int64_t slices = (int64_t)p->B * p->Hkv;
   s.M = rows > 64 && slices * ((rows + 127) / 128) >= 256 ? 128 : 32;
+  s.resident = s.M == 128 && resident_bytes(p) <= kLds;
+  if (s.resident) s.M = 32;
   s.QB = (rows + s.M - 1) / s.M;
   s.n_split = 1;
   s.split_keys = p->Lk;
-  if (s.M == 32) {
+  if (s.M == 32 && !s.resident) {
     const int64_t tiles = slices * s.QB, want = (1024 + tiles - 1) / tiles;
     const int most = (p->Lk + 127) / 128;
     int n = (int)(want < most ? want : most);
@@ -99,6 +109,25 @@ static int launch_d(const FwdArgs& a, int occ128, hipStream_t stream) {
                           fwd_lds_bytes<128, D, NMODE_CROSS>(), a, occ128, stream, nullptr, occ[0]);
   return launch_variant(fgattn_fwd_kernel<32, D, NMODE_CROSS, 2, PART_ALL, false, 2, 2, 1>,
                         fwd_lds_bytes<32, D, NMODE_CROSS, false, 2, 2, 1>(), a, occ128, stream, nullptr, occ[1], 0, 64);
+}
+
+template <int D, int WV>
+static int launch_resident(const CrossArgs& a, int lds, int cus, hipStream_t stream) {
+  static std::mutex mutex;
+  static bool ready[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return FGATTN_E_DEVICE;
+  {
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!ready[dev]) {
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(cross_kernel<D, WV>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) !=
+          hipSuccess)
+        return FGATTN_E_DEVICE;
+      ready[dev] = true;
+    }
+  }
+  hipLaunchKernelGGL((cross_kernel<D, WV>), dim3(a.tiles < cus ? a.tiles : cus), dim3(WV * 64), lds, stream, a);
+  return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;
 }
 
 }  // namespace fgx
@@ -160,6 +189,17 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
   a.lazy_raw = fg::kLazyLog2 / a.c_log2;
   a.scale_abs = sabs;
   a.q_sign = p->scale < 0.0f ? 0x80008000u : 0u;
+  if (s.resident) {
+    fgx::CrossArgs c = {};
+    c.q = a.q; c.k = a.k; c.v = a.v; c.out = a.out; c.lse = lse;
+    c.q_lens = q_lens; c.k_lens = k_lens;
+    c.q_sb = a.q_sb; c.q_sh = a.q_sh; c.q_sl = a.q_sl; c.k_sb = a.k_sb; c.k_sh = a.k_sh; c.k_sl = a.k_sl;
+    c.v_sb = a.v_sb; c.v_sh = a.v_sh; c.v_sl = a.v_sl; c.o_sb = a.o_sb; c.o_sh = a.o_sh; c.o_sl = a.o_sl;
+    c.Hkv = p->Hkv; c.group = a.group; c.Lq = p->Lq; c.Lk = p->Lk; c.rows = a.L; c.QB = s.QB; c.tiles = (int32_t)s.items;
+    c.c_log2 = a.c_log2; c.lazy_raw = a.lazy_raw; c.scale_abs = a.scale_abs; c.q_sign = a.q_sign;
+    const int lds = fgx::resident_bytes(p);
+    return p->d == 64 ? fgx::launch_resident<64, 12>(c, lds, cus, stream) : fgx::launch_resident<128, 8>(c, lds, cus, stream);
+  }
   rc = p->d == 64 ? fgx::launch_d<64>(a, cus, stream) : fgx::launch_d<128>(a, cus, stream);
   if (rc || s.n_split == 1) return rc;
   fgx::JoinArgs j = {};

@@ -1,0 +1,306 @@
+// Cross attention, forward, many query rows: K and V of a key head stay in LDS while the waves of a workgroup go through
+// its query tiles.
+//
+// A workgroup owns a range of the 32-row query tiles of all key heads (the same number for every workgroup, one workgroup per
+// compute unit).  For each key head of its range it loads the head's K and V into LDS once; then every wave takes every WV-th
+// tile and meets no barrier until the key head changes.  A wave's work is one software pipeline over (query tile, key tile)
+// that does not end with the query tile: step n runs the matrix products O += V(n-1)^T P(n-1)^T and S(n+1) = K(n+1) Q^T side by side with the
+// exponentials of S(n), where n+1 may be the first key tile of the next query tile, whose rows have been loaded meanwhile, and n-1 the
+// last one of the tile before, whose result is then stored.  With 8 key tiles per query tile, starting and ending a pipeline for each
+// took 7.2 of 15.6 us.
+#pragma once
+#include "fgattn_fwd.hpp"
+
+namespace fgx {
+
+using namespace fg;
+
+struct CrossArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  float* lse;
+  const int32_t *q_lens, *k_lens;
+  int64_t q_sb, q_sh, q_sl, k_sb, k_sh, k_sl, v_sb, v_sh, v_sl, o_sb, o_sh, o_sl;
+  int32_t Hkv, group, Lq, Lk, rows, QB, tiles;   // rows = group * Lq of a key head; QB = tiles of 32 of them; tiles of all
+  float c_log2, lazy_raw, scale_abs;
+  uint32_t q_sign;
+};
+
+// One 1 KiB load of the wave into LDS (see gather16_first), with a base that may just have been moved to scalar registers by
+// vector instructions: five wait states before the load reads it.
+__device__ __forceinline__ void gather16(const void* base, unsigned byte_off, unsigned lds_base) {
+  base = pin_scalar(base);
+  lds_base = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_base);
+  asm volatile(
+      "s_mov_b32 m0, %2 ; fg_m0\n\t"
+      "s_nop 4\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(byte_off), "s"(base), "s"(lds_base)
+      : "memory", "m0");
+}
+
+// A row of the result from a transposed accumulator (lane (g, row): elements 8 r4 + 4 g .. + 3 of every block): the lanes of a pair
+// exchange halves, so that each stores 16 bytes and a row gets 32 in a run (with 8 bytes per lane twice the stores).
+template <int D>
+__device__ __forceinline__ void store_row16(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int g, bool valid) {
+  i32x4 out[D / 16];
+#pragma unroll
+  for (int db = 0; db < D / 32; db++)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; r4 += 2) {
+      unsigned w[2][2];
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const f32x2 f = {acc[db][4 * (r4 + h) + 2 * e] * factor, acc[db][4 * (r4 + h) + 2 * e + 1] * factor};
+          w[h][e] = __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
+        }
+      auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+      auto hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+      out[2 * db + r4 / 2] = i32x4{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+    }
+  if (valid) {
+#pragma unroll
+    for (int i = 0; i < D / 16; i++) *reinterpret_cast<i32x4*>(row + 16 * i + 8 * g) = out[i];
+  }
+}
+
+template <int D, int WV>
+__global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs a) {
+  constexpr int CH = D / 8, ROWB = D * 2, RPI = 64 / CH, TB = 32 * ROWB, SSTEPS = D / 16, DBLK = D / 32, NE = SSTEPS;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // key tile t: K at 2 t TB, V at (2 t + 1) TB
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned lds0 = lds_address(smem);
+  // LDS layout and reader's offsets: as in fgattn_fwd.hpp
+  const int u = (lane >> 4) & 1, kq = (lane & 15) >> 2, qq = lane & 3;
+  const int kor = (ln * ROWB) | ((g ^ (D == 128 ? (ln & 15) : ((ln >> 1) & 7))) << 4);
+  const int vsw = D == 128 ? (kq << 2) : (((kq >> 1) & 1) << 2);
+  int voff[DBLK];
+#pragma unroll
+  for (int db = 0; db < DBLK; db++) voff[db] = (4 * g + kq) * ROWB + ((qq & 1) << 3) + ((((4 * db) ^ vsw) + 2 * u + (qq >> 1)) << 4);
+  const int lrow = lane / CH, pc = lane % CH;
+
+  // workgroups of one XCD take neighbouring ranges
+  const int G = gridDim.x, per = G >> 3, rem = G & 7, x = blockIdx.x & 7;
+  const int64_t me = x * per + min(x, rem) + (blockIdx.x >> 3);
+  int tile = (int)(a.tiles * me / G);
+  const int tile_end = (int)(a.tiles * (me + 1) / G);
+
+  f32x16 O[DBLK], SA, SB;
+  i32x4 PA[2], PB[2];
+  bf16x8 qf[SSTEPS];
+  i32x4 qn[SSTEPS];
+
+  bool again = false;
+  while (tile < tile_end) {   // one key head
+    const int slice = tile / a.QB, first = tile - slice * a.QB;
+    const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
+    const int n_here = min(a.QB - first, tile_end - tile);
+    tile += n_here;
+    const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
+    const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+    const int nt = ((k_len + 63) >> 6) * 2;   // (an even number: scores and probabilities of even and odd tiles have registers of their own)
+    // (with one query head per key head the rows behind a shorter sequence are whole tiles at the end)
+    const int last = min(first + n_here, a.group == 1 ? (q_len + 31) >> 5 : a.QB);
+    const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh;
+    const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh;
+    if (again) __syncthreads();   // every wave is done with the head before
+    again = true;
+    // rows past the last key are read as the last one: finite wherever the tensor is, and masked out
+    for (int i = wv; i < nt * (32 / RPI); i += WV) {
+      const int r = i * RPI + lrow, key = min(r, k_len - 1), rt = r & 31;
+      const unsigned kx = (unsigned)((pc ^ (D == 128 ? (rt & 15) : ((rt >> 1) & 7))) << 4);
+      const unsigned vx = (unsigned)((pc ^ (D == 128 ? ((rt & 3) << 2) : (((rt >> 1) & 1) << 2))) << 4);
+      const int t = i / (32 / RPI);
+      const unsigned at = lds0 + t * 2 * TB + (i - t * (32 / RPI)) * RPI * ROWB;
+      gather16(kbase, __umul24((unsigned)key, (unsigned)(a.k_sl * 2)) + kx, at);
+      gather16(vbase, __umul24((unsigned)key, (unsigned)(a.v_sl * 2)) + vx, at + TB);
+    }
+    wait_vmem_all();
+    __syncthreads();
+
+    int j = first + wv;
+    if (j >= last) continue;
+    const uint16_t* const qbase = a.q + b * a.q_sb + (int64_t)hk * a.group * a.q_sh;
+    uint16_t* const obase = a.out + b * a.o_sb + (int64_t)hk * a.group * a.o_sh;
+    // this lane's row of query tile jj: whether it counts, its head inside the group and its token
+    auto place = [&](int jj, int& head, int& pos) -> bool {
+      const int row = min(jj * 32 + ln, a.rows - 1);
+      head = 0;
+      if (a.group > 1) head = (int)((unsigned)row / (unsigned)a.Lq);
+      pos = row - head * a.Lq;
+      return jj * 32 + ln < a.rows && pos < q_len;
+    };
+    auto load_q = [&](int jj) {
+      int head, pos;
+      place(jj, head, pos);
+      const char* qp = reinterpret_cast<const char*>(qbase + head * a.q_sh + (int64_t)pos * a.q_sl) + 16 * g;
+#pragma unroll
+      for (int s = 0; s < SSTEPS; s++) qn[s] = *reinterpret_cast<const i32x4*>(qp + 32 * s);
+    };
+    auto take_q = [&]() {
+#pragma unroll
+      for (int s = 0; s < SSTEPS; s++) qf[s] = __builtin_bit_cast(bf16x8, qn[s] ^ (int)a.q_sign);
+    };
+    float m_run = -INFINITY, m_pend = -INFINITY, neg_mc = 0.0f, l_run = 0.0f, l_run2 = 0.0f;
+    auto set_base = [&](float m) {
+      m_run = m;
+      neg_mc = m == -INFINITY ? 0.0f : -m * a.c_log2;
+    };
+    auto finish = [&](int jj, float m, float l) {
+      int head, pos;
+      const bool valid = place(jj, head, pos);
+      const float l_tot = lane_pair_sum(l);
+      const float inv = l_tot > 0.0f ? 1.0f / l_tot : 0.0f;
+      store_row16<D>(obase + head * a.o_sh + (int64_t)pos * a.o_sl, O, inv, g, valid);
+      if (valid && g == 0) a.lse[(int64_t)slice * a.rows + jj * 32 + ln] = l_tot > 0.0f ? a.scale_abs * m + __logf(l_tot) : -INFINITY;
+    };
+    auto clear_o = [&]() {
+#pragma unroll
+      for (int db = 0; db < DBLK; db++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) O[db][r] = 0.0f;
+    };
+    clear_o();
+    if (k_len == 0) {
+      for (; j < last; j += WV) finish(j, -INFINITY, 0.0f);
+      continue;
+    }
+    // scores of key tile t that do not count
+    auto mask = [&](int t, f32x16& S) {
+      const int limit = k_len - 32 * t;
+      if (__builtin_expect(limit < 32, 0)) mask_drop(S, (limit <= 0 ? ~0u : ~0u << limit) >> (4 * g));
+    };
+    constexpr int AHEAD = 3;
+    auto read_kf = [&](int base, int s) {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + (base ^ (32 * s))));
+    };
+    auto read_vf = [&](int base, int e) {
+      const int db = e >> 1, c = e & 1;
+      const unsigned char* p0 = smem + base + voff[db] + (16 * c) * ROWB;
+      s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FG_LDS s16x4*)(p0));
+      s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FG_LDS s16x4*)(p0 + 8 * ROWB));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    load_q(j);
+    take_q();
+#pragma unroll
+    for (int r = 0; r < 16; r++) SA[r] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NE; s++) SA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_kf(kor, s), qf[s], SA, 0, 0, 0);
+    mask(0, SA);
+#pragma unroll
+    for (int c = 0; c < 2; c++) PB[c] = i32x4{0, 0, 0, 0};
+    float l_new, l_new2, m_lane;
+    // O += V^T P^T of V tile tv, Sn = K Q^T of key tile tk, P = exp(So - m)
+    auto step = [&](int tv, int tk, const i32x4 (&Pin)[2], const f32x16& So, i32x4 (&Pout)[2], f32x16& Sn) {
+      int kb = kor + tk * (2 * TB), vb = tv * (2 * TB) + TB;
+      asm volatile("" : "+v"(kb));   // (one addition here, and plain XORs with constants below)
+      bf16x8 kf[NE], vf[NE];
+#pragma unroll
+      for (int e = 0; e < AHEAD; e++) {
+        kf[e] = read_kf(kb, e);
+        vf[e] = read_vf(vb, e);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; r++) Sn[r] = 0.0f;
+      const bf16x8 pin[2] = {__builtin_bit_cast(bf16x8, Pin[0]), __builtin_bit_cast(bf16x8, Pin[1])};
+      constexpr int VPS = 16 / NE;
+      l_new = l_run;
+      l_new2 = l_run2;
+      m_lane = m_pend;
+#pragma unroll
+      for (int e = 0; e < NE; e++) {
+        if (e + AHEAD < NE) vf[e + AHEAD] = read_vf(vb, e + AHEAD);
+        O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[e], pin[e & 1], O[e >> 1], 0, 0, 0);
+        if (e + AHEAD < NE) kf[e + AHEAD] = read_kf(kb, e + AHEAD);
+        Sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[e], qf[e], Sn, 0, 0, 0);
+#pragma unroll
+        for (int y = 0; y < VPS; y += 2) {
+          const int r = e * VPS + y;
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r], a.c_log2, neg_mc));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r + 1], a.c_log2, neg_mc));
+          l_new += p0;
+          l_new2 += p1;
+          m_lane = max3(m_lane, So[r], So[r + 1]);
+          f32x2 pp = {p0, p1};
+          int pk = __builtin_bit_cast(int, __builtin_convertvector(pp, bf16x2));
+          asm volatile("" : "+v"(pk));   // keeps the compiler from sinking the conversion out of the slot
+          Pout[r >> 3][(r & 7) >> 1] = pk;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // the exponent base moves where a running max has passed it by more than lazy_raw: the tile's exponentials are formed again, O and
+    // the sums rescaled
+    auto settle = [&](const f32x16& So, i32x4 (&Pout)[2]) {
+      m_pend = lane_pair_max(m_lane);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(m_pend > m_run + a.lazy_raw) != 0, 0)) {
+#pragma clang fp contract(off)
+        const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - m_pend) * a.c_log2);
+        set_base(m_pend);
+        l_new = l_run * alpha;
+        l_new2 = l_run2 * alpha;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r], a.c_log2, neg_mc));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r + 1], a.c_log2, neg_mc));
+          l_new += p0;
+          l_new2 += p1;
+          f32x2 pp = {p0, p1};
+          Pout[r >> 3][(r & 7) >> 1] = __builtin_bit_cast(int, __builtin_convertvector(pp, bf16x2));
+        }
+#pragma unroll
+        for (int db = 0; db < DBLK; db++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) O[db][r] *= alpha;
+      }
+      l_run = l_new;
+      l_run2 = l_new2;
+    };
+    // S of key tile 0 is in SA, P of the tile before (the last of the query tile before) in PB
+    int j_prev = -1;
+    for (;;) {
+      const float m_prev = m_run, l_prev = l_run + l_run2;
+      m_pend = row_max(SA);
+      set_base(m_pend);
+      l_run = l_run2 = 0.0f;
+      load_q(j + WV < last ? j + WV : j);
+      step(nt - 1, 1, PB, SA, PA, SB);
+      if (j_prev >= 0) finish(j_prev, m_prev, l_prev);
+      clear_o();
+      l_run = l_new;
+      l_run2 = l_new2;
+      mask(1, SB);
+      int t = 1;
+#pragma unroll 1
+      for (; t < nt - 1; t += 2) {
+        step(t - 1, t + 1, PA, SB, PB, SA);
+        settle(SB, PB);
+        mask(t + 1, SA);
+        step(t, t + 2, PB, SA, PA, SB);
+        settle(SA, PA);
+        mask(t + 2, SB);
+      }
+      take_q();   // (after the last tile: once more that tile's, for nothing)
+      step(nt - 2, 0, PA, SB, PB, SA);
+      settle(SB, PB);
+      mask(0, SA);
+      j_prev = j;
+      j += WV;
+      if (j >= last) break;
+    }
+    {
+      const int vb = (nt - 1) * 2 * TB + TB;
+      const bf16x8 pin[2] = {__builtin_bit_cast(bf16x8, PB[0]), __builtin_bit_cast(bf16x8, PB[1])};
+#pragma unroll
+      for (int e = 0; e < NE; e++) O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_vf(vb, e), pin[e & 1], O[e >> 1], 0, 0, 0);
+      finish(j_prev, m_run, l_run + l_run2);
+    }
+  }
+}
+
+}  // namespace fgx

@@ -6,6 +6,7 @@ not been built, importing a symbol from it raises.
 """
 import ctypes
 import os
+import struct
 
 from . import build as _build
 
@@ -259,46 +260,64 @@ def fgattn_grid_size(params):
 
 # ---- rotary positions, norms of queries and keys, cross attention ----
 # These bindings also compare every tensor with the params (the C ABI sees pointers only) and run on the tensors' own device,
-# whichever is current.
+# whichever is current.  Small calls take as long as this file does, so the comparisons are made in one loop and the
+# params are packed as bytes.
+
+_ROPE_FIELDS, _CROSS_FIELDS = struct.Struct("9if12q"), struct.Struct("6i24qfi")
+
 
 def _refuse(code):
     raise FgattnError(code)
 
 
-def _pointer(t, device, dtype, shape=None, strides=None):
-    """Address of a tensor (None: NULL) on `device`, of `dtype` and, if given, of this shape (contiguous) or these strides."""
-    if t is None:
-        return None
-    if t.device != device:
+def _addresses(device, tensors):
+    """Addresses of tensors (None: NULL) given as (tensor, dtype, shape, strides or None where it has to be contiguous), all on device
+    number `device`."""
+    found = []
+    for t, dtype, shape, strides in tensors:
+        if t is None:
+            found.append(None)
+            continue
+        if t.dtype is not dtype or t.get_device() != device or t.shape != shape or \
+                (not t.is_contiguous() if strides is None else t.stride() != strides):
+            _compare(t, device, dtype, shape, strides)
+        found.append(t.data_ptr())
+    return found
+
+
+def _compare(t, device, dtype, shape, strides):
+    """Refuses a tensor that differs from what the params say (the stride of a dimension of one does not matter)."""
+    if t.get_device() != device:
         _refuse(E_DEVICE)
     if t.dtype is not dtype:
         _refuse(E_DTYPE)
-    if shape is not None and (t.shape != shape or (strides is None and not t.is_contiguous())):
+    if t.shape != shape or (strides is None and not t.is_contiguous()):
         _refuse(E_SHAPE)
-    if strides is not None and t.stride() != strides and any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), strides)):
+    if strides is not None and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
         _refuse(E_STRIDE)
-    return t.data_ptr()
 
 
-def _launch(device, stream, tensors, call):
-    """call(stream pointer) with `device` current; a stream of another device is refused, and the allocator learns of tensors
-    that are used on a stream other than the current one."""
+def _launch(call, args, device, stream, tensors):
+    """call(*args, stream) with device number `device` current; a stream of another device is refused, and the allocator learns
+    of tensors that are used on a stream other than the current one."""
     import torch
-    if device.type != "cuda":
+    if device < 0:
         _refuse(E_DEVICE)
-    if device.index != torch.cuda.current_device():
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _launch(device, stream, tensors, call)
+            return _launch(call, args, device, stream, tensors)
     if stream is None:
         stream = torch.cuda.current_stream()
     else:
-        if stream.device != device:
+        if stream.device.index != device:
             _refuse(E_DEVICE)
         if stream != torch.cuda.current_stream():
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
-    _check(call(ctypes.c_void_p(stream.cuda_stream)))
+    rc = call(*args, stream.cuda_stream)
+    if rc != 0:
+        raise FgattnError(rc)
 
 
 def fgattn_rope_table(axes, cos, sin, mscale=1.0, stream=None):
@@ -308,65 +327,78 @@ def fgattn_rope_table(axes, cos, sin, mscale=1.0, stream=None):
     n = len(axes)
     if not 1 <= n <= 3:
         _refuse(E_SHAPE)
-    table = (FgattnRopeAxis * n)(*[FgattnRopeAxis(*x, *(0.0, 1.0, 1.0, 0.0, 32.0, 1.0)[len(x) - 3:]) for x in axes])
-    rows, pairs = 1, 0
-    for x in table:
-        rows, pairs = rows * x.size, pairs + x.pairs
-    c, s = (_pointer(t, cos.device, torch.float32, (rows, pairs)) for t in (cos, sin))
-    _launch(cos.device, stream, (cos, sin), lambda st: lib().fgattn_rope_table(table, n, mscale, c, s, st))
+    rows, pairs, table = 1, 0, []
+    for x in axes:
+        rows, pairs = rows * x[0], pairs + x[1]
+        table.append(FgattnRopeAxis(*x, *(0.0, 1.0, 1.0, 0.0, 32.0, 1.0)[len(x) - 3:]))
+    device, f32, shape = cos.get_device(), torch.float32, (rows, pairs)
+    c, s = _addresses(device, ((cos, f32, shape, None), (sin, f32, shape, None)))
+    _launch(lib().fgattn_rope_table, ((FgattnRopeAxis * n)(*table), n, mscale, c, s), device, stream, (cos, sin))
+
+
+_DTYPES = {}
 
 
 def _dtype_code(dtype):
-    import torch
-    code = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}.get(dtype)
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32})
+    code = _DTYPES.get(dtype)
     return _refuse(E_DTYPE) if code is None else code
 
 
 def make_rope_params(q, k, q_out, k_out, rot_dims, layout=ROPE_INTERLEAVED, eps=1e-6, flags=FLAG_ROPE_NORM):
     """fgattn_rope_params for [B, H, L, d] tensors (any strides with a contiguous last dim); k and k_out may be None.  For the
     backward call q_out and k_out are the gradients that come in, and dq and dk have the strides of q and k."""
-    B, Hq, L, d = q.shape
-    for t in (q, k, q_out, k_out):
-        if t is not None and (t.dim() != 4 or t.stride(3) != 1):
-            _refuse(E_STRIDE)
-    if q_out.shape != q.shape or (k is None) != (k_out is None) or \
-            (k is not None and (k.shape != k_out.shape or (k.shape[0], k.shape[2], k.shape[3]) != (B, L, d))):
+    shape, Hk = q.shape, 0
+    if len(shape) != 4 or q_out.shape != shape or (k is None) != (k_out is None):
         _refuse(E_SHAPE)
-    none = (0, 0, 0)
-    return FgattnRopeParams(B, Hq, 0 if k is None else k.shape[1], L, d, rot_dims, layout, _dtype_code(q.dtype), flags, eps,
-                            *q.stride()[:3], *(none if k is None else k.stride()[:3]), *q_out.stride()[:3],
-                            *(none if k is None else k_out.stride()[:3]))
+    B, Hq, L, d = shape
+    a, c = q.stride(), q_out.stride()
+    b = e = (0, 0, 0, 1)
+    if k is not None:
+        shape = k.shape
+        if len(shape) != 4 or shape[0] != B or shape[2] != L or shape[3] != d or k_out.shape != shape:
+            _refuse(E_SHAPE)
+        Hk, b, e = shape[1], k.stride(), k_out.stride()
+    if a[3] != 1 or b[3] != 1 or c[3] != 1 or e[3] != 1:
+        _refuse(E_STRIDE)
+    return FgattnRopeParams.from_buffer_copy(_ROPE_FIELDS.pack(
+        B, Hq, Hk, L, d, rot_dims, layout, _dtype_code(q.dtype), flags, eps, *a[:3], *b[:3], *c[:3], *e[:3]))
 
 
 def fgattn_rope_workspace_bytes(params):
     return int(lib().fgattn_rope_workspace_bytes(ctypes.byref(params)))
 
 
-def _rope_pointers(p, q, k, cos, sin, positions, q_weight, k_weight, device, dtype):
+def _rope_operands(params, q, k, cos, sin, positions, q_weight, k_weight, results, backward, dtype, device):
+    """Addresses of q, k, weights, cos, sin, positions and `results` (forward: q_out, k_out; backward: dq_out, dk_out, dq, dk), and the
+    table's rows."""
     import torch
-    if _dtype_code(dtype) != p.dtype:
+    B, Hq, Hk, L, d, rot, _, code, flags, _, *s = _ROPE_FIELDS.unpack_from(params)
+    if _dtype_code(dtype) != code:
         _refuse(E_DTYPE)
-    f32 = torch.float32
     if (cos is None) != (sin is None):
         _refuse(E_NULL)
-    w_type = f32 if p.flags & FLAG_ROPE_WEIGHT_FP32 else dtype
+    f32 = torch.float32
+    w_type = f32 if flags & FLAG_ROPE_WEIGHT_FP32 else dtype
     rows = 0 if cos is None else cos.shape[0]
-    table = (rows, p.rot_dims // 2)
-    return [_pointer(q, device, dtype, (p.B, p.Hq, p.L, p.d), (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
-            _pointer(k, device, dtype, (p.B, p.Hk, p.L, p.d), (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
-            _pointer(q_weight, device, w_type, (p.d,)), _pointer(k_weight, device, w_type, (p.d,)),
-            _pointer(cos, device, f32, table), _pointer(sin, device, f32, table), rows,
-            _pointer(positions, device, torch.int32, (p.B, p.L)), ctypes.byref(p)]
+    of_q, of_k, weight, table = (B, Hq, L, d), (B, Hk, L, d), (d,), (rows, rot // 2)
+    sq, sk = (s[0], s[1], s[2], 1), (s[3], s[4], s[5], 1)
+    given = [(q, dtype, of_q, sq), (k, dtype, of_k, sk), (q_weight, w_type, weight, None), (k_weight, w_type, weight, None),
+             (cos, f32, table, None), (sin, f32, table, None), (positions, torch.int32, (B, L), None),
+             (results[0], dtype, of_q, (s[6], s[7], s[8], 1)), (results[1], dtype, of_k, (s[9], s[10], s[11], 1))]
+    if backward:
+        given += [(results[2], dtype, of_q, sq), (results[3], dtype, of_k, sk)]
+    return _addresses(device, given), rows
 
 
 def fgattn_rope_forward(q, k, params, q_out, k_out, cos=None, sin=None, positions=None, q_weight=None, k_weight=None, stream=None):
     """Queries and keys normed per head and turned by their positions (see include/fgattn.h)."""
-    p, dev, dt = params, q.device, q.dtype
-    args = _rope_pointers(p, q, k, cos, sin, positions, q_weight, k_weight, dev, dt)
-    args += [_pointer(q_out, dev, dt, (p.B, p.Hq, p.L, p.d), (p.qo_stride_b, p.qo_stride_h, p.qo_stride_l, 1)),
-             _pointer(k_out, dev, dt, (p.B, p.Hk, p.L, p.d), (p.ko_stride_b, p.ko_stride_h, p.ko_stride_l, 1))]
-    _launch(dev, stream, (q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight),
-            lambda st: lib().fgattn_rope_forward(*args, st))
+    device = q.get_device()
+    a, rows = _rope_operands(params, q, k, cos, sin, positions, q_weight, k_weight, (q_out, k_out), False, q.dtype, device)
+    _launch(lib().fgattn_rope_forward, (*a[:6], rows, a[6], ctypes.byref(params), a[7], a[8]), device, stream,
+            (q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight))
 
 
 def fgattn_rope_backward(q, k, params, dq_out, dk_out, dq, dk, cos=None, sin=None, positions=None, q_weight=None, k_weight=None,
@@ -374,23 +406,18 @@ def fgattn_rope_backward(q, k, params, dq_out, dk_out, dq, dk, cos=None, sin=Non
     """Gradients of fgattn_rope_forward: dq, dk and, where given, dq_weight and dk_weight (fp32).  q and k may be None without
     FLAG_ROPE_NORM."""
     import torch
-    p, dev, dt = params, dq_out.device, dq_out.dtype
-    args = _rope_pointers(p, q, k, cos, sin, positions, q_weight, k_weight, dev, dt)
-    shape_q, shape_k = (p.B, p.Hq, p.L, p.d), (p.B, p.Hk, p.L, p.d)
-    args += [_pointer(dq_out, dev, dt, shape_q, (p.qo_stride_b, p.qo_stride_h, p.qo_stride_l, 1)),
-             _pointer(dk_out, dev, dt, shape_k, (p.ko_stride_b, p.ko_stride_h, p.ko_stride_l, 1)),
-             _pointer(dq, dev, dt, shape_q, (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
-             _pointer(dk, dev, dt, shape_k, (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
-             _pointer(dq_weight, dev, torch.float32, (p.d,)), _pointer(dk_weight, dev, torch.float32, (p.d,)),
-             *_workspace(workspace, dev)]
-    _launch(dev, stream, (q, k, dq_out, dk_out, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, workspace),
-            lambda st: lib().fgattn_rope_backward(*args, st))
+    device, f32, weight = dq_out.get_device(), torch.float32, (params.d,)
+    a, rows = _rope_operands(params, q, k, cos, sin, positions, q_weight, k_weight, (dq_out, dk_out, dq, dk), True, dq_out.dtype,
+                             device)
+    dw = _addresses(device, ((dq_weight, f32, weight, None), (dk_weight, f32, weight, None)))
+    _launch(lib().fgattn_rope_backward, (*a[:6], rows, a[6], ctypes.byref(params), *a[7:], *dw, *_scratch(workspace, device)), device, stream,
+            (q, k, dq_out, dk_out, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, workspace))
 
 
-def _workspace(workspace, device):
+def _scratch(workspace, device):
     if workspace is None:
         return None, 0
-    if workspace.device != device:
+    if workspace.get_device() != device:
         _refuse(E_DEVICE)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
@@ -398,21 +425,21 @@ def _workspace(workspace, device):
 def make_cross_params(q, k, v, out, scale, dout=None, dq=None, dk=None, dv=None):
     """fgattn_cross_params for q, out [B, H, Lq, d] and k, v [B, Hkv, Lk, d] (any strides with a contiguous last dim); for the
     backward call also the incoming gradient and the three gradients."""
-    B, H, Lq, d = q.shape
-    Hkv, Lk = k.shape[1], k.shape[2]
+    of_q, of_k = q.shape, k.shape
+    if len(of_q) != 4 or len(of_k) != 4 or of_k[0] != of_q[0] or of_k[3] != of_q[3]:
+        _refuse(E_SHAPE)
     strides = []
-    for t, shape in ((q, q.shape), (k, (B, Hkv, Lk, d)), (v, (B, Hkv, Lk, d)), (out, q.shape), (dout, q.shape), (dq, q.shape),
-                     (dk, (B, Hkv, Lk, d)), (dv, (B, Hkv, Lk, d))):
+    for t, shape in ((q, of_q), (k, of_k), (v, of_k), (out, of_q), (dout, of_q), (dq, of_q), (dk, of_k), (dv, of_k)):
         if t is None:
             strides += (0, 0, 0)
             continue
         if t.shape != shape:
             _refuse(E_SHAPE)
         s = t.stride()
-        if len(s) != 4 or s[3] != 1:
+        if s[3] != 1:
             _refuse(E_STRIDE)
         strides += s[:3]
-    return FgattnCrossParams(B, H, Hkv, Lq, Lk, d, *strides, scale, 0)
+    return FgattnCrossParams.from_buffer_copy(_CROSS_FIELDS.pack(of_q[0], of_q[1], of_k[1], of_q[2], of_k[2], of_q[3], *strides, scale, 0))
 
 
 def fgattn_cross_workspace_bytes(params):
@@ -426,31 +453,34 @@ def fgattn_cross_backward_workspace_bytes(params):
 def fgattn_cross_forward(q, k, v, params, out, lse, workspace=None, q_lens=None, k_lens=None, stream=None):
     """Attention of q's tokens to k and v, another sequence with its own lengths (see include/fgattn.h)."""
     import torch
-    p, dev, bf16 = params, q.device, torch.bfloat16
-    shape_q, shape_k = (p.B, p.H, p.Lq, p.d), (p.B, p.Hkv, p.Lk, p.d)
-    args = [_pointer(q, dev, bf16, shape_q, (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
-            _pointer(k, dev, bf16, shape_k, (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
-            _pointer(v, dev, bf16, shape_k, (p.v_stride_b, p.v_stride_h, p.v_stride_l, 1)),
-            _pointer(q_lens, dev, torch.int32, (p.B,)), _pointer(k_lens, dev, torch.int32, (p.B,)), ctypes.byref(p),
-            _pointer(out, dev, bf16, shape_q, (p.o_stride_b, p.o_stride_h, p.o_stride_l, 1)),
-            _pointer(lse, dev, torch.float32, shape_q[:3]), *_workspace(workspace, dev)]
-    _launch(dev, stream, (q, k, v, out, lse, workspace, q_lens, k_lens), lambda st: lib().fgattn_cross_forward(*args, st))
+    device, bf16, i32 = q.get_device(), torch.bfloat16, torch.int32
+    B, H, Hkv, Lq, Lk, d, *s = _CROSS_FIELDS.unpack_from(params)
+    of_q, of_k, lens = (B, H, Lq, d), (B, Hkv, Lk, d), (B,)
+    a = _addresses(device, ((q, bf16, of_q, (s[0], s[1], s[2], 1)),
+                            (k, bf16, of_k, (s[3], s[4], s[5], 1)),
+                            (v, bf16, of_k, (s[6], s[7], s[8], 1)),
+                            (q_lens, i32, lens, None), (k_lens, i32, lens, None),
+                            (out, bf16, of_q, (s[9], s[10], s[11], 1)),
+                            (lse, torch.float32, of_q[:3], None)))
+    _launch(lib().fgattn_cross_forward, (*a[:5], ctypes.byref(params), a[5], a[6], *_scratch(workspace, device)), device, stream,
+            (q, k, v, out, lse, workspace, q_lens, k_lens))
 
 
 def fgattn_cross_backward(q, k, v, out, lse, dout, params, dq, dk, dv, workspace, q_lens=None, k_lens=None, stream=None):
     """Gradients of fgattn_cross_forward with respect to q, k and v, from its inputs and results and the gradient of out."""
     import torch
-    p, dev, bf16 = params, q.device, torch.bfloat16
-    shape_q, shape_k = (p.B, p.H, p.Lq, p.d), (p.B, p.Hkv, p.Lk, p.d)
-    args = [_pointer(q, dev, bf16, shape_q, (p.q_stride_b, p.q_stride_h, p.q_stride_l, 1)),
-            _pointer(k, dev, bf16, shape_k, (p.k_stride_b, p.k_stride_h, p.k_stride_l, 1)),
-            _pointer(v, dev, bf16, shape_k, (p.v_stride_b, p.v_stride_h, p.v_stride_l, 1)),
-            _pointer(out, dev, bf16, shape_q, (p.o_stride_b, p.o_stride_h, p.o_stride_l, 1)),
-            _pointer(lse, dev, torch.float32, shape_q[:3]),
-            _pointer(dout, dev, bf16, shape_q, (p.do_stride_b, p.do_stride_h, p.do_stride_l, 1)),
-            _pointer(q_lens, dev, torch.int32, (p.B,)), _pointer(k_lens, dev, torch.int32, (p.B,)), ctypes.byref(p),
-            _pointer(dq, dev, bf16, shape_q, (p.dq_stride_b, p.dq_stride_h, p.dq_stride_l, 1)),
-            _pointer(dk, dev, bf16, shape_k, (p.dk_stride_b, p.dk_stride_h, p.dk_stride_l, 1)),
-            _pointer(dv, dev, bf16, shape_k, (p.dv_stride_b, p.dv_stride_h, p.dv_stride_l, 1)), *_workspace(workspace, dev)]
-    _launch(dev, stream, (q, k, v, out, lse, dout, dq, dk, dv, workspace, q_lens, k_lens),
-            lambda st: lib().fgattn_cross_backward(*args, st))
+    device, bf16, i32 = q.get_device(), torch.bfloat16, torch.int32
+    B, H, Hkv, Lq, Lk, d, *s = _CROSS_FIELDS.unpack_from(params)
+    of_q, of_k, lens = (B, H, Lq, d), (B, Hkv, Lk, d), (B,)
+    a = _addresses(device, ((q, bf16, of_q, (s[0], s[1], s[2], 1)),
+                            (k, bf16, of_k, (s[3], s[4], s[5], 1)),
+                            (v, bf16, of_k, (s[6], s[7], s[8], 1)),
+                            (out, bf16, of_q, (s[9], s[10], s[11], 1)),
+                            (lse, torch.float32, of_q[:3], None),
+                            (dout, bf16, of_q, (s[12], s[13], s[14], 1)),
+                            (q_lens, i32, lens, None), (k_lens, i32, lens, None),
+                            (dq, bf16, of_q, (s[15], s[16], s[17], 1)),
+                            (dk, bf16, of_k, (s[18], s[19], s[20], 1)),
+                            (dv, bf16, of_k, (s[21], s[22], s[23], 1))))
+    _launch(lib().fgattn_cross_backward, (*a[:8], ctypes.byref(params), *a[8:], *_scratch(workspace, device)), device, stream,
+            (q, k, v, out, lse, dout, dq, dk, dv, workspace, q_lens, k_lens))
