@@ -1,11 +1,13 @@
 // Cross attention, forward: the tokens of a layer attend to an encoder's states.
 //
-// The tile kernel is the dense forward kernel's (fgattn_fwd.hpp, NMODE_CROSS): keys in order, the key side with a length of
-// its own.  The query heads that share a key head are laid below each other (group * Lq rows), so that a tile is full
-// whether a call has many tokens or a single one of many heads.  Calls with many rows run 128-row tiles; their bound is the
-// matrix pipe.  Calls with few rows run 32-row tiles in single-wave workgroups, each against a range of the keys; their
-// bound is reading K and V once, which takes as many waves in flight as LDS holds.  A second kernel joins the
-// ranges: with m_s, l_s, O_s of range s, out = sum O_s e^(m_s - m) / sum l_s e^(m_s - m).
+// The query heads that share a key head are laid below each other (group * Lq rows), so that tiles of 32 rows are full whether a
+// call has many tokens or a single one of many heads.  Two ways through the keys (plan_of says which):
+//   many tiles   cross_kernel (fgcross_fwd.hpp): a workgroup of eight or twelve waves keeps a key head's K and V in LDS, or passes them
+//                through rings there, while each wave goes through tiles of its own; the bound is the matrix pipe, or reading
+//                Q and writing the result where keys are few.
+//   few tiles    the dense forward kernel of fgattn_fwd.hpp (NMODE_CROSS), single-wave workgroups, each against a range of the
+//                keys; the bound is reading K and V once, which takes as many waves in flight as LDS holds.  join_kernel
+//                joins the ranges: with m_s, l_s, O_s of range s, out = sum O_s e^(m_s - m) / sum l_s e^(m_s - m).
 #include <mutex>
 
 #include "fgattn_fwd.hpp"
@@ -17,7 +19,9 @@ namespace fgx {
 
 using namespace fg;
 
-// One wave per query row: lane s holds range s's weight, then the wave goes through the ranges' rows of d floats.
+// A workgroup per query row.  Every wave has all ranges' weights in its lanes and adds up every fourth range's row; the four sums
+// meet in LDS.  Bound: latency.  With one wave per row and its loads one after the other 64 ranges of eight rows took 20 us
+// more.
 constexpr int kMaxSplits = 64;
 struct JoinArgs {
   const float* part_o;
@@ -26,69 +30,100 @@ struct JoinArgs {
   float* lse;
   const int32_t* q_lens;
   int64_t o_sb, o_sh, o_sl;
-  int32_t Hkv, Lq, rows, group, QB, M, n_split, n_rows;   // rows = group * Lq; n_rows of all slices
+  int32_t Hkv, Lq, rows, group, QB, n_split;   // rows = group * Lq
   float c_log2, scale_abs;
 };
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const JoinArgs a) {
   constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= a.n_rows) return;
-  const int slice = (int)(at / a.rows), row = (int)(at - (int64_t)slice * a.rows);
+  __shared__ float sums[4][D];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int slice = (int)(blockIdx.x / (unsigned)a.rows), row = (int)(blockIdx.x - (unsigned)slice * (unsigned)a.rows);
   const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
   const int of_group = row / a.Lq, l = row - of_group * a.Lq;
   if (a.q_lens && l >= a.q_lens[b]) return;
-  const int tile = row / a.M;
-  const int64_t first = ((int64_t)slice * a.QB + tile) * a.n_split * a.M + (row - tile * a.M);   // range s: + s * M
+  const int64_t first = ((int64_t)slice * a.QB + (row >> 5)) * a.n_split * 32 + (row & 31);   // range s: + 32 s
   float m = -INFINITY, l_s = 0.0f;
   if (lane < a.n_split) {
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * (first + (int64_t)lane * a.M));
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * (first + (int64_t)lane * 32));
     m = ml[0];
     l_s = ml[1];
+  }
+  const float* src = a.part_o + first * D + lane * E;
+  float part[kMaxSplits / 4][E];
+#pragma unroll
+  for (int n = 0; n < kMaxSplits / 4; n++) {
+    const int s = min(4 * n + wv, a.n_split - 1);
+    if (4 * n < a.n_split) {
+#pragma unroll
+      for (int e = 0; e < E; e++) part[n][e] = src[(int64_t)s * 32 * D + e];
+    }
   }
   float top = m;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  const float w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * a.c_log2);
+  const float w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * a.c_log2);   // (0 in the lanes behind the last range)
   float total = l_s * w;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
   float o[E] = {};
-  for (int s = 0; s < a.n_split; s++) {
-    const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
-    const float* src = a.part_o + (first + (int64_t)s * a.M) * D + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; e++) o[e] += ws * src[e];
+  for (int n = 0; n < kMaxSplits / 4; n++) {
+    if (4 * n >= a.n_split) break;
+    const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), __builtin_amdgcn_readfirstlane(4 * n + wv)));
+#pragma unroll
+    for (int e = 0; e < E; e++) o[e] += ws * part[n][e];
   }
-  const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-  __bf16* dst = reinterpret_cast<__bf16*>(a.out + b * a.o_sb + (int64_t)(hk * a.group + of_group) * a.o_sh + (int64_t)l * a.o_sl) + lane * E;
 #pragma unroll
-  for (int e = 0; e < E; e++) dst[e] = (__bf16)(o[e] * inv);
-  if (lane == 0) a.lse[at] = total > 0.0f ? a.scale_abs * top + __logf(total) : -INFINITY;
+  for (int e = 0; e < E; e++) sums[wv][lane * E + e] = o[e];
+  __syncthreads();
+  if (tid >= D / 4) return;
+  const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+  f32x4 f = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int n = 0; n < 4; n++) f += *reinterpret_cast<const f32x4*>(&sums[n][4 * tid]);
+  f *= inv;
+  uint16_t* dst = a.out + b * a.o_sb + (int64_t)(hk * a.group + of_group) * a.o_sh + (int64_t)l * a.o_sl + 4 * tid;
+  *reinterpret_cast<i32x2*>(dst) = __builtin_bit_cast(i32x2, __builtin_convertvector(f, bf16x4));
+  if (tid == 0) a.lse[blockIdx.x] = total > 0.0f ? a.scale_abs * top + __logf(total) : -INFINITY;
 }
 
 // LDS of a key head's tiles (K and V, 32 keys each) and how many tiles a workgroup can hold.
-constexpr int kLds = 160 * 1024;
-static int resident_bytes(const fgattn_cross_params* p) { return (p->Lk + 63) / 64 * 64 * 4 * p->d; }
+static int64_t resident_bytes(const fgattn_cross_params* p) { return ((int64_t)p->Lk + 63) / 64 * 64 * 4 * p->d; }
 
 struct Plan {
-  bool resident;
-  int M, QB, n_split, split_keys;
-  int64_t items;
+  bool tiles, stream;   // cross_kernel; its keys pass through rings
+  int QB, unit;         // tiles of a key head; cross_kernel: tiles that go to one workgroup together
+  int n_split, split_keys;
+  int64_t items;        // without cross_kernel
 };
-static Plan plan_of(const fgattn_cross_params* p) {
+constexpr int kWaves128 = 8, kWaves64 = 12, kWavesRings = 8;
+static Plan plan_of(const fgattn_cross_params* p, int cus) {
   Plan s;
   const int rows = p->H / p->Hkv * p->Lq;
   const int64_t slices = (int64_t)p->B * p->Hkv;
-  s.M = rows > 64 && slices * ((rows + 127) / 128) >= 256 ? 128 : 32;
-  s.resident = s.M == 128 && resident_bytes(p) <= kLds;
-  if (s.resident) s.M = 32;
-  s.QB = (rows + s.M - 1) / s.M;
+  s.QB = (rows + 31) / 32;
+  const int64_t tiles = slices * s.QB;
+  s.stream = resident_bytes(p) > kLdsBytes;
+  // Which way (microseconds of cross_kernel against ranges; 32 to 8192 keys and 8 to 2520 tiles measured).  Keys in LDS: 77 keys
+  // 24 x 1000 tokens 9.6 against 9.4, 12 x 4096 12.7 against 17.1; 226 keys 8 x 64 tokens 9.0 against 9.8, 24 x 1000 11.6
+  // against 50.  Keys through rings, where few tiles' waves take as long as many: 512 keys 12 x 512 tokens 20.5 against 23, 2048
+  // keys 12 x 1000 tokens 54 against 53, 8192 keys 12 x 1000 tokens 197 against 132 and 24 x 1000 198 against 225; d = 64, 2048 keys
+  // 12 x 1000 tokens 40 against 36, 8192 keys 24 x 1000 141 against 110 and 12 x 4096 143 against 162: as many tiles as the root of the
+  // keys asks for.
+  s.tiles = s.stream ? tiles * tiles * p->d >= 9000 * (int64_t)p->Lk : p->Lk <= 160 ? tiles * p->d >= 128 * 1024 : true;
   s.n_split = 1;
   s.split_keys = p->Lk;
-  if (s.M == 32 && !s.resident) {
-    const int64_t tiles = slices * s.QB, want = (1024 + tiles - 1) / tiles;
+  s.items = tiles;
+  // Units of cross_kernel: a tile, or with rings, where the waves go through the keys together, one for every wave.  Where a wave has no
+  // more than one tile, as many as leave no workgroup with tiles of two key heads, whose K and V it would have to
+  // wait for twice (226 keys, 12 x 1000 tokens).
+  const int waves = s.stream ? kWavesRings : p->d == 64 ? kWaves64 : kWaves128;
+  s.unit = s.stream ? waves : 1;
+  const int64_t groups = cus / slices;
+  if (groups >= 1 && (s.QB + groups - 1) / groups <= waves) s.unit = (int)((s.QB + groups - 1) / groups);
+  if (!s.tiles) {
+    const int64_t want = (1024 + tiles - 1) / tiles;
     const int most = (p->Lk + 127) / 128;
     int n = (int)(want < most ? want : most);
     if (n > kMaxSplits) n = kMaxSplits;
@@ -96,23 +131,13 @@ static Plan plan_of(const fgattn_cross_params* p) {
       s.split_keys = ((p->Lk + n - 1) / n + 31) / 32 * 32;
       s.n_split = (p->Lk + s.split_keys - 1) / s.split_keys;
     }
+    s.items = tiles * s.n_split;
   }
-  s.items = slices * s.QB * s.n_split;
   return s;
 }
 
-template <int D>
-static int launch_d(const FwdArgs& a, int occ128, hipStream_t stream) {
-  static int occ[2][64];
-  if (a.M == 128)
-    return launch_variant(fgattn_fwd_kernel<128, D, NMODE_CROSS, D == 64 ? 3 : 2, PART_ALL, false, 2, 2, 4, true>,
-                          fwd_lds_bytes<128, D, NMODE_CROSS>(), a, occ128, stream, nullptr, occ[0]);
-  return launch_variant(fgattn_fwd_kernel<32, D, NMODE_CROSS, 2, PART_ALL, false, 2, 2, 1>,
-                        fwd_lds_bytes<32, D, NMODE_CROSS, false, 2, 2, 1>(), a, occ128, stream, nullptr, occ[1], 0, 64);
-}
-
-template <int D, int WV>
-static int launch_resident(const CrossArgs& a, int lds, int cus, hipStream_t stream) {
+template <int D, int WV, bool STREAM>
+static int launch_cross(const CrossArgs& a, int lds, int cus, hipStream_t stream) {
   static std::mutex mutex;
   static bool ready[64];
   int dev = 0;
@@ -120,14 +145,21 @@ static int launch_resident(const CrossArgs& a, int lds, int cus, hipStream_t str
   {
     std::lock_guard<std::mutex> lock(mutex);
     if (!ready[dev]) {
-      if (hipFuncSetAttribute(reinterpret_cast<const void*>(cross_kernel<D, WV>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) !=
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(cross_kernel<D, WV, STREAM>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes) !=
           hipSuccess)
         return FGATTN_E_DEVICE;
       ready[dev] = true;
     }
   }
-  hipLaunchKernelGGL((cross_kernel<D, WV>), dim3(a.tiles < cus ? a.tiles : cus), dim3(WV * 64), lds, stream, a);
+  hipLaunchKernelGGL((cross_kernel<D, WV, STREAM>), dim3(a.units < cus ? a.units : cus), dim3(WV * 64), lds, stream, a);
   return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;
+}
+
+template <int D>
+static int launch_ranges(const FwdArgs& a, int cus, hipStream_t stream) {
+  static int occ[64];
+  return launch_variant(fgattn_fwd_kernel<32, D, NMODE_CROSS, 2, PART_ALL, false, 2, 2, 1>,
+                        fwd_lds_bytes<32, D, NMODE_CROSS, false, 2, 2, 1>(), a, cus, stream, nullptr, occ, 0, 64);
 }
 
 }  // namespace fgx
@@ -136,8 +168,8 @@ extern "C" {
 
 size_t fgattn_cross_workspace_bytes(const fgattn_cross_params* p) {
   if (fgx::check_shape(p) != FGATTN_OK) return 0;
-  const fgx::Plan s = fgx::plan_of(p);
-  return s.n_split > 1 ? ((size_t)s.items * s.M * (p->d + 2) * sizeof(float) + 255) & ~(size_t)255 : 0;
+  const fgx::Plan s = fgx::plan_of(p, 1);   // (how many compute units there are does not matter to the ranges)
+  return s.n_split > 1 ? ((size_t)s.items * 32 * (p->d + 2) * sizeof(float) + 255) & ~(size_t)255 : 0;
 }
 
 int fgattn_cross_forward(const void* q, const void* k, const void* v, const int32_t* q_lens, const int32_t* k_lens,
@@ -156,7 +188,7 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
   int cus = 0;
   if ((rc = fg::require_device(&cus))) return rc;
   hipStream_t stream = static_cast<hipStream_t>(stream_v);
-  const fgx::Plan s = fgx::plan_of(p);
+  const fgx::Plan s = fgx::plan_of(p, cus);
   fg::FwdArgs a = {};
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -174,14 +206,14 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
   a.Lk = p->Lk;
   a.q_lens = q_lens;
   a.k_lens = k_lens;
-  a.M = s.M;
+  a.M = 32;
   a.N = 1;
   a.QB = s.QB;
   a.n_items = (int32_t)s.items;
   a.n_split = s.n_split;
   a.split_keys = s.split_keys;
   a.part_o = static_cast<float*>(workspace);
-  a.part_ml = a.part_o + s.items * s.M * p->d;
+  a.part_ml = a.part_o + s.items * 32 * p->d;
   a.schedule = fg::SCHED_DIRECT;
   const float sabs = fabsf(p->scale);
   a.c_log2 = sabs * 1.44269504088896340736f;
@@ -189,18 +221,25 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
   a.lazy_raw = fg::kLazyLog2 / a.c_log2;
   a.scale_abs = sabs;
   a.q_sign = p->scale < 0.0f ? 0x80008000u : 0u;
-  if (s.resident) {
+  if (s.tiles) {
     fgx::CrossArgs c = {};
     c.q = a.q; c.k = a.k; c.v = a.v; c.out = a.out; c.lse = lse;
     c.q_lens = q_lens; c.k_lens = k_lens;
     c.q_sb = a.q_sb; c.q_sh = a.q_sh; c.q_sl = a.q_sl; c.k_sb = a.k_sb; c.k_sh = a.k_sh; c.k_sl = a.k_sl;
     c.v_sb = a.v_sb; c.v_sh = a.v_sh; c.v_sl = a.v_sl; c.o_sb = a.o_sb; c.o_sh = a.o_sh; c.o_sl = a.o_sl;
-    c.Hkv = p->Hkv; c.group = a.group; c.Lq = p->Lq; c.Lk = p->Lk; c.rows = a.L; c.QB = s.QB; c.tiles = (int32_t)s.items;
+    c.Hkv = p->Hkv; c.group = a.group; c.Lq = p->Lq; c.Lk = p->Lk; c.rows = a.L; c.QB = s.QB;
+    c.unit = s.unit;
+    c.QU = (s.QB + c.unit - 1) / c.unit;
+    c.units = p->B * p->Hkv * c.QU;
     c.c_log2 = a.c_log2; c.lazy_raw = a.lazy_raw; c.scale_abs = a.scale_abs; c.q_sign = a.q_sign;
-    const int lds = fgx::resident_bytes(p);
-    return p->d == 64 ? fgx::launch_resident<64, 12>(c, lds, cus, stream) : fgx::launch_resident<128, 8>(c, lds, cus, stream);
+    if (s.stream)
+      return p->d == 64 ? fgx::launch_cross<64, fgx::kWavesRings, true>(c, fgx::kLdsBytes, cus, stream)
+                        : fgx::launch_cross<128, fgx::kWavesRings, true>(c, fgx::kLdsBytes, cus, stream);
+    const int lds = (int)fgx::resident_bytes(p);
+    return p->d == 64 ? fgx::launch_cross<64, fgx::kWaves64, false>(c, lds, cus, stream)
+                      : fgx::launch_cross<128, fgx::kWaves128, false>(c, lds, cus, stream);
   }
-  rc = p->d == 64 ? fgx::launch_d<64>(a, cus, stream) : fgx::launch_d<128>(a, cus, stream);
+  rc = p->d == 64 ? fgx::launch_ranges<64>(a, cus, stream) : fgx::launch_ranges<128>(a, cus, stream);
   if (rc || s.n_split == 1) return rc;
   fgx::JoinArgs j = {};
   j.part_o = a.part_o;
@@ -214,12 +253,10 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
   j.rows = a.L;
   j.group = a.group;
   j.QB = s.QB;
-  j.M = s.M;
   j.n_split = s.n_split;
-  j.n_rows = p->B * p->H * p->Lq;
   j.c_log2 = a.c_log2;
   j.scale_abs = sabs;
-  const dim3 grid((unsigned)((j.n_rows + 3) / 4));
+  const dim3 grid((unsigned)p->B * p->H * p->Lq);
   if (p->d == 64) hipLaunchKernelGGL(fgx::join_kernel<64>, grid, dim3(256), 0, stream, j);
   else hipLaunchKernelGGL(fgx::join_kernel<128>, grid, dim3(256), 0, stream, j);
   return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;

@@ -1,8 +1,8 @@
 // Cross attention, forward, many query rows: K and V of a key head stay in LDS while the waves of a workgroup go through
 // its query tiles.
 //
-// A workgroup owns a range of the 32-row query tiles of all key heads (the same number for every workgroup, one workgroup per
-// compute unit).  For each key head of its range it loads the head's K and V into LDS once; then every wave takes every WV-th
+// A workgroup owns a range of the 32-row query tiles of all key heads (as near as can be the same number for every workgroup, one
+// workgroup per compute unit).  For each key head of its range it loads the head's K and V into LDS once; then every wave takes every WV-th
 // tile and meets no barrier until the key head changes.  A wave's work is one software pipeline over (query tile, key tile)
 // that does not end with the query tile: step n runs the matrix products O += V(n-1)^T P(n-1)^T and S(n+1) = K(n+1) Q^T side by side with the
 // exponentials of S(n), where n+1 may be the first key tile of the next query tile, whose rows have been loaded meanwhile, and n-1 the
@@ -15,13 +15,16 @@ namespace fgx {
 
 using namespace fg;
 
+constexpr int kLdsBytes = 160 * 1024;
+
 struct CrossArgs {
   const uint16_t *q, *k, *v;
   uint16_t* out;
   float* lse;
   const int32_t *q_lens, *k_lens;
   int64_t q_sb, q_sh, q_sl, k_sb, k_sh, k_sl, v_sb, v_sh, v_sl, o_sb, o_sh, o_sl;
-  int32_t Hkv, group, Lq, Lk, rows, QB, tiles;   // rows = group * Lq of a key head; QB = tiles of 32 of them; tiles of all
+  int32_t Hkv, group, Lq, Lk, rows, QB;   // rows = group * Lq of a key head; QB = tiles of 32 of them
+  int32_t unit, QU, units;                // workgroups share out units of `unit` tiles: QU of a key head, units of all
   float c_log2, lazy_raw, scale_abs;
   uint32_t q_sign;
 };
@@ -67,10 +70,14 @@ __device__ __forceinline__ void store_row16(uint16_t* row, const f32x16 (&acc)[D
   }
 }
 
-template <int D, int WV>
+template <int D, int WV, bool STREAM>
 __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs a) {
   constexpr int CH = D / 8, ROWB = D * 2, RPI = 64 / CH, TB = 32 * ROWB, SSTEPS = D / 16, DBLK = D / 32, NE = SSTEPS;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // key tile t: K at 2 t TB, V at (2 t + 1) TB
+  // Pairs of key tiles.  Resident: pair p's K and V in slot p.  STREAM: rings of SLOTS slots, K's and V's.
+  constexpr int PB2 = 2 * TB, SLOTS = kLdsBytes / (2 * PB2), K_STEP = STREAM ? PB2 : 2 * PB2, V_OFF = STREAM ? SLOTS * PB2 : PB2;
+  constexpr int IPW = 64 / RPI / WV;   // STREAM: loads of a wave for a pair of tiles of K or V
+  static_assert(!STREAM || (IPW * RPI * WV == 64 && SLOTS >= 3), "every wave fetches the same number of rows");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned lds0 = lds_address(smem);
@@ -86,8 +93,8 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
   // workgroups of one XCD take neighbouring ranges
   const int G = gridDim.x, per = G >> 3, rem = G & 7, x = blockIdx.x & 7;
   const int64_t me = x * per + min(x, rem) + (blockIdx.x >> 3);
-  int tile = (int)(a.tiles * me / G);
-  const int tile_end = (int)(a.tiles * (me + 1) / G);
+  int at_unit = (int)(a.units * me / G);
+  const int end_unit = (int)(a.units * (me + 1) / G);
 
   f32x16 O[DBLK], SA, SB;
   i32x4 PA[2], PB[2];
@@ -95,35 +102,64 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
   i32x4 qn[SSTEPS];
 
   bool again = false;
-  while (tile < tile_end) {   // one key head
-    const int slice = tile / a.QB, first = tile - slice * a.QB;
+  while (at_unit < end_unit) {   // one key head
+    const int slice = at_unit / a.QU, first_unit = at_unit - slice * a.QU, first = first_unit * a.unit;
     const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
-    const int n_here = min(a.QB - first, tile_end - tile);
-    tile += n_here;
+    const int n_here = min(a.QU - first_unit, end_unit - at_unit);
+    at_unit += n_here;
     const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
     const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
     const int nt = ((k_len + 63) >> 6) * 2;   // (an even number: scores and probabilities of even and odd tiles have registers of their own)
     // (with one query head per key head the rows behind a shorter sequence are whole tiles at the end)
-    const int last = min(first + n_here, a.group == 1 ? (q_len + 31) >> 5 : a.QB);
+    const int last = min(first + n_here * a.unit, a.group == 1 ? (q_len + 31) >> 5 : a.QB);
     const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh;
     const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh;
     if (again) __syncthreads();   // every wave is done with the head before
     again = true;
-    // rows past the last key are read as the last one: finite wherever the tensor is, and masked out
-    for (int i = wv; i < nt * (32 / RPI); i += WV) {
-      const int r = i * RPI + lrow, key = min(r, k_len - 1), rt = r & 31;
-      const unsigned kx = (unsigned)((pc ^ (D == 128 ? (rt & 15) : ((rt >> 1) & 7))) << 4);
-      const unsigned vx = (unsigned)((pc ^ (D == 128 ? ((rt & 3) << 2) : (((rt >> 1) & 1) << 2))) << 4);
-      const int t = i / (32 / RPI);
-      const unsigned at = lds0 + t * 2 * TB + (i - t * (32 / RPI)) * RPI * ROWB;
-      gather16(kbase, __umul24((unsigned)key, (unsigned)(a.k_sl * 2)) + kx, at);
-      gather16(vbase, __umul24((unsigned)key, (unsigned)(a.v_sl * 2)) + vx, at + TB);
+    // Rows r .. of pair `pair` of K or V -> LDS.  Rows past the last key are read as the last one: finite wherever the tensor is, and
+    // masked out.
+    auto fetch = [&](const uint16_t* base, unsigned row_bytes, bool is_k, int pair, int r, unsigned at) {
+      const int key = min(pair * 64 + r + lrow, k_len - 1), rt = r + lrow;
+      const unsigned swz = D == 128 ? (is_k ? rt & 15 : (rt & 3) << 2) : (is_k ? (rt >> 1) & 7 : ((rt >> 1) & 1) << 2);
+      gather16(base, __umul24((unsigned)key, row_bytes) + ((pc ^ swz) << 4), at + r * ROWB);
+    };
+    const unsigned k_rowb = (unsigned)(a.k_sl * 2), v_rowb = (unsigned)(a.v_sl * 2);
+    const int np = nt >> 1;
+    int k_next = 0, v_next = 0, k_slot = 0, v_slot = 0;   // STREAM: the pairs that are fetched next and the slots they go to
+    // this wave's load i of the next pair of K / V; the last one moves on
+    auto fetch_k = [&](int i) {
+      fetch(kbase, k_rowb, true, k_next, (wv * IPW + i) * RPI, lds0 + k_slot * PB2);
+      if (i + 1 < IPW) return;
+      k_next = k_next + 1 == np ? 0 : k_next + 1;
+      k_slot = k_slot + 1 == SLOTS ? 0 : k_slot + 1;
+    };
+    auto fetch_v = [&](int i) {
+      fetch(vbase, v_rowb, false, v_next, (wv * IPW + i) * RPI, lds0 + V_OFF + v_slot * PB2);
+      if (i + 1 < IPW) return;
+      v_next = v_next + 1 == np ? 0 : v_next + 1;
+      v_slot = v_slot + 1 == SLOTS ? 0 : v_slot + 1;
+    };
+    if constexpr (STREAM) {
+      if (np > 0) {
+        for (int n = 0; n + 1 < SLOTS; n++)
+          for (int i = 0; i < 2 * IPW; i++)
+            if (i < IPW) fetch_k(i);
+            else fetch_v(i - IPW);
+      }
+    } else {
+      for (int i = wv; i < np * (64 / RPI); i += WV) {
+        const int pair = i / (64 / RPI), r = (i - pair * (64 / RPI)) * RPI;
+        fetch(kbase, k_rowb, true, pair, r, lds0 + pair * K_STEP);
+        fetch(vbase, v_rowb, false, pair, r, lds0 + pair * K_STEP + V_OFF);
+      }
     }
     wait_vmem_all();
     __syncthreads();
 
     int j = first + wv;
-    if (j >= last) continue;
+    // STREAM: the waves go through the keys together, a wave without a tile of its own along with the others
+    const int turns = (last - first + WV - 1) / WV;
+    if (STREAM ? turns <= 0 : j >= last) continue;
     const uint16_t* const qbase = a.q + b * a.q_sb + (int64_t)hk * a.group * a.q_sh;
     uint16_t* const obase = a.out + b * a.o_sb + (int64_t)hk * a.group * a.o_sh;
     // this lane's row of query tile jj: whether it counts, its head inside the group and its token
@@ -132,7 +168,7 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       head = 0;
       if (a.group > 1) head = (int)((unsigned)row / (unsigned)a.Lq);
       pos = row - head * a.Lq;
-      return jj * 32 + ln < a.rows && pos < q_len;
+      return jj * 32 + ln < a.rows && pos < q_len && (!STREAM || jj < last);
     };
     auto load_q = [&](int jj) {
       int head, pos;
@@ -174,6 +210,8 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       const int limit = k_len - 32 * t;
       if (__builtin_expect(limit < 32, 0)) mask_drop(S, (limit <= 0 ? ~0u : ~0u << limit) >> (4 * g));
     };
+    using of_v = std::integral_constant<int, 1>;
+    using of_k = std::integral_constant<int, 2>;
     constexpr int AHEAD = 3;
     auto read_kf = [&](int base, int s) {
       return __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + (base ^ (32 * s))));
@@ -195,9 +233,12 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
 #pragma unroll
     for (int c = 0; c < 2; c++) PB[c] = i32x4{0, 0, 0, 0};
     float l_new, l_new2, m_lane;
-    // O += V^T P^T of V tile tv, Sn = K Q^T of key tile tk, P = exp(So - m)
-    auto step = [&](int tv, int tk, const i32x4 (&Pin)[2], const f32x16& So, i32x4 (&Pout)[2], f32x16& Sn) {
-      int kb = kor + tk * (2 * TB), vb = tv * (2 * TB) + TB;
+    // O += V^T P^T with V's tile at v_at of LDS, Sn = K Q^T with K's tile at k_at, P = exp(So - m).  STREAM: FETCH = 1 / 2 also
+    // fetches this wave's rows of the next pair of V / K, between the matrix instructions: a load holds the wave until the memory
+    // path has taken it, while those already issued go on.
+    auto step = [&](auto fetch_c, int v_at, int k_at, const i32x4 (&Pin)[2], const f32x16& So, i32x4 (&Pout)[2], f32x16& Sn) {
+      constexpr int FETCH = decltype(fetch_c)::value;
+      int kb = kor + k_at, vb = v_at;
       asm volatile("" : "+v"(kb));   // (one addition here, and plain XORs with constants below)
       bf16x8 kf[NE], vf[NE];
 #pragma unroll
@@ -212,8 +253,8 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       l_new = l_run;
       l_new2 = l_run2;
       m_lane = m_pend;
-#pragma unroll
-      for (int e = 0; e < NE; e++) {
+      auto slot = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
         if (e + AHEAD < NE) vf[e + AHEAD] = read_vf(vb, e + AHEAD);
         O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[e], pin[e & 1], O[e >> 1], 0, 0, 0);
         if (e + AHEAD < NE) kf[e + AHEAD] = read_kf(kb, e + AHEAD);
@@ -231,8 +272,13 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
           asm volatile("" : "+v"(pk));   // keeps the compiler from sinking the conversion out of the slot
           Pout[r >> 3][(r & 7) >> 1] = pk;
         }
+        if constexpr (STREAM && e % (NE / 2) == 1 && e / (NE / 2) < IPW) {
+          if constexpr (FETCH == 1) fetch_v(e / (NE / 2));
+          else fetch_k(e / (NE / 2));
+        }
         __builtin_amdgcn_sched_barrier(0);
-      }
+      };
+      [&]<int... E>(std::integer_sequence<int, E...>) { (slot(std::integral_constant<int, E>()), ...); }(std::make_integer_sequence<int, NE>());
     };
     // the exponent base moves where a running max has passed it by more than lazy_raw: the tile's exponentials are formed again, O and
     // the sums rescaled
@@ -261,43 +307,62 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       l_run = l_new;
       l_run2 = l_new2;
     };
+    // Where the next two steps find their tiles: V's pair p and K's pair p + 1, or of the next query tile's first.  STREAM: K(p+1) and
+    // V(p) have arrived (what was fetched in the three rounds before this one may still be under way), every wave is
+    // done with K(p) and V(p-1), and the pairs SLOTS and SLOTS - 1 ahead follow into their slots.
+    int k_at = 0, v_at = V_OFF;
+    bool v_first = true;
+    auto advance = [&](int p) {
+      if constexpr (STREAM) {
+        wait_vmem_le<(SLOTS - 2) * 2 * IPW>();
+        __syncthreads();
+        k_at = k_at + PB2 == SLOTS * PB2 ? 0 : k_at + PB2;
+        if (v_first) v_first = false;
+        else v_at = v_at + PB2 == V_OFF + SLOTS * PB2 ? V_OFF : v_at + PB2;
+      } else {
+        v_at = p * K_STEP + V_OFF;
+        k_at = p + 1 == np ? 0 : (p + 1) * K_STEP;
+      }
+    };
     // S of key tile 0 is in SA, P of the tile before (the last of the query tile before) in PB
     int j_prev = -1;
-    for (;;) {
+    for (int turn = 0;;) {
       const float m_prev = m_run, l_prev = l_run + l_run2;
       m_pend = row_max(SA);
       set_base(m_pend);
       l_run = l_run2 = 0.0f;
       load_q(j + WV < last ? j + WV : j);
-      step(nt - 1, 1, PB, SA, PA, SB);
+      step(of_k(), v_at + TB, k_at + TB, PB, SA, PA, SB);
       if (j_prev >= 0) finish(j_prev, m_prev, l_prev);
       clear_o();
       l_run = l_new;
       l_run2 = l_new2;
       mask(1, SB);
-      int t = 1;
 #pragma unroll 1
-      for (; t < nt - 1; t += 2) {
-        step(t - 1, t + 1, PA, SB, PB, SA);
+      for (int p = 0; p + 1 < np; p++) {
+        advance(p);
+        step(of_v(), v_at, k_at, PA, SB, PB, SA);
         settle(SB, PB);
-        mask(t + 1, SA);
-        step(t, t + 2, PB, SA, PA, SB);
+        mask(2 * p + 2, SA);
+        step(of_k(), v_at + TB, k_at + TB, PB, SA, PA, SB);
         settle(SA, PA);
-        mask(t + 2, SB);
+        mask(2 * p + 3, SB);
       }
+      advance(np - 1);
       take_q();   // (after the last tile: once more that tile's, for nothing)
-      step(nt - 2, 0, PA, SB, PB, SA);
+      step(of_v(), v_at, k_at, PA, SB, PB, SA);
       settle(SB, PB);
       mask(0, SA);
       j_prev = j;
       j += WV;
-      if (j >= last) break;
+      turn++;
+      if (STREAM ? turn == turns : j >= last) break;
     }
+    if constexpr (STREAM) wait_vmem_all();   // (pairs that nobody reads; none may land after this workgroup)
     {
-      const int vb = (nt - 1) * 2 * TB + TB;
       const bf16x8 pin[2] = {__builtin_bit_cast(bf16x8, PB[0]), __builtin_bit_cast(bf16x8, PB[1])};
 #pragma unroll
-      for (int e = 0; e < NE; e++) O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_vf(vb, e), pin[e & 1], O[e >> 1], 0, 0, 0);
+      for (int e = 0; e < NE; e++) O[e >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_vf(v_at + TB, e), pin[e & 1], O[e >> 1], 0, 0, 0);
       finish(j_prev, m_run, l_run + l_run2);
     }
   }

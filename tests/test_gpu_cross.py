@@ -54,6 +54,12 @@ CASES = [
     (1, 16, 2, 1111, 512, 64, "bhld", None, None, None),
     (1, 40, 1, 900, 1, 128, "bhld", None, None, None),
     (1, 3, 1, 70, 4100, 128, "bhld", None, None, None),
+    (2, 12, 1, 1500, 517, 128, "blhd", None, [1500, 1211], [517, 3]),     # many rows, keys beyond what LDS holds: rings
+    (3, 6, 2, 1111, 641, 128, "bhld", None, [1111, 1, 600], [384, 641, 0]),
+    (1, 9, 4, 1111, 1030, 64, "slice", -0.15, None, None),
+    (2, 9, 2, 999, 661, 64, "blhd", None, None, [661, 64]),
+    (1, 24, 1, 3001, 320, 128, "bhld", None, None, [289]),                # all of LDS
+    (2, 17, 1, 1301, 640, 64, "bhld", None, [1301, 1300], [640, 577]),
 ]
 IDS = ["-".join(str(x) for x in c[:7]) for c in CASES]
 
