@@ -2,11 +2,14 @@
 //   dV = P^T dO,  dP = dO V^T,  dS = P (dP - D),  dQ = scale dS K,  dK = scale dS^T Q.
 // Two kernels, each of which forms S and dP again (14 d flop per score instead of 10): neither needs atomics, so results are the
 // same bits every time.
-//   dq_kernel    a wave owns 32 query rows (Q and dO in registers, one query per lane); the keys stream through LDS.
-//                It also forms D and leaves (lse, D) of every row for the second kernel.
+//   dq_kernel    a wave owns 32 query rows (Q and dO in registers, one query per lane) and goes through the keys, which lie in LDS
+//                (as in fgcross_fwd.hpp: one key head's K and V for all of a workgroup's tiles, or rings).  It also forms D and
+//                leaves (lse, D) of every row for the second kernel.  D comes from the bf16 result, whose rounding shows in dP - D where
+//                a row has few keys (a relative error of dQ of 0.0026 with 77 keys and 0.0036 with 3, against 0.0024 with the exact
+//                D): with up to kOwnDelta keys it is the sum of P dP over a first pass through the keys, and the result is not read.  With few rows and many keys the keys are split over
+//                workgroups, whose fp32 partial sums are added up in a fixed order by a kernel of their own.
 //   dkdv_kernel  a wave owns 32 keys (K in registers, one key per lane, its V rows in LDS); the queries stream through LDS.  With few
-//                keys and many queries the query rows are split over workgroups, whose fp32 partial sums a third kernel adds up in
-//                a fixed order.
+//                keys and many queries the query rows are split over workgroups, and the partial sums added up likewise.
 // Both contractions over a streamed tile read it twice: row-wise (A operand of S or dP) and transposed (A operand of the
 // product that sums over its rows, ds_read_b64_tr_b16).  P and dS are rounded to bf16 as the matrix instructions' operands.
 #include <mutex>
@@ -25,10 +28,13 @@ struct BwdArgs {
   const int32_t *q_lens, *k_lens;
   float* stats;     // [B][H][Lq][2]: lse in log2 units, D
   float* part;      // dkdv_kernel with several ranges of rows: [n_split][slice][Lk][2][d]
+  float* part_q;    // dq_kernel with several ranges of keys: [k_split][B][H][Lq][d]
   int64_t q_sb, q_sh, q_sl, k_sb, k_sh, k_sl, v_sb, v_sh, v_sl, o_sb, o_sh, o_sl;
   int64_t do_sb, do_sh, do_sl, dq_sb, dq_sh, dq_sl, dk_sb, dk_sh, dk_sl, dv_sb, dv_sh, dv_sl;
   int32_t B, H, Hkv, group, Lq, Lk;
-  int32_t n_items, QB, KB, n_split, units, units_per_split;   // KB: key tiles of a slice; units: 32-row tiles of a key head's rows
+  int32_t n_items, KB, n_split, units, units_per_split;   // dkdv_kernel; KB: key tiles of a slice; units: 32-row tiles of a key head's rows
+  int32_t rows, QB, unit, QU, dq_units, k_split, split_keys;   // dq_kernel (as CrossArgs); ranges of split_keys keys
+  int32_t own_delta;                                           // dq_kernel forms D from P and dP and does not read the result
   float scale, c_log2;
 };
 
@@ -115,106 +121,257 @@ __device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D /
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(256, 2) dq_kernel(const BwdArgs a) {
+// A wave's work on a query tile is a software pipeline over its key tiles: step n runs S(n+1) = K(n+1) Q^T and dP(n+1) = V(n+1) dO^T side by
+// side with the exponentials and products that make dS(n) of S(n) and dP(n), then dQ += K(n)^T dS(n)^T.  Bound: the matrix
+// pipe (24 instructions per tile) beside about 90 vector instructions.  The next query tile's rows are not loaded ahead: there
+// are no registers left for them, and the other wave of the SIMD computes meanwhile.
+template <int D, bool STREAM>
+__global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
   using T = Tile<D>;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * T::BYTES];   // K and V, two slots each
+  constexpr int WV = 8, TB = T::BYTES, RPI = T::RPI, NE = T::SSTEPS, DBLK = T::DBLK;
+  // pairs of key tiles: slot s holds 64 rows of K, then 64 of V
+  constexpr int PB2 = 2 * TB, SLOTS = kLdsBytes / (2 * PB2), IPW = 64 / RPI / WV;
+  static_assert(IPW * RPI * WV == 64 && SLOTS >= 4, "every wave fetches the same number of rows");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int w = xcd_item(a.n_items);
-  const int slice = w / a.QB, qi = w - slice * a.QB;
-  const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
-  const int rows = a.group * a.Lq;
-  const int my_row = qi * 128 + wv * 32 + ln;
-  const int row = min(my_row, rows - 1);
-  const int of_group = (int)((unsigned)row / (unsigned)a.Lq), pos = row - of_group * a.Lq;
-  const int head = hk * a.group + of_group;
-  const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
-  const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
-  const bool counts = my_row < rows && pos < q_len && k_len > 0;
-
-  bf16x8 qf[T::SSTEPS], dof[T::SSTEPS];
-  float delta = 0.0f;
-  {
-    const char* qp = reinterpret_cast<const char*>(a.q + b * a.q_sb + head * a.q_sh + (int64_t)pos * a.q_sl);
-    const char* op = reinterpret_cast<const char*>(a.o + b * a.o_sb + head * a.o_sh + (int64_t)pos * a.o_sl);
-    const char* dp = reinterpret_cast<const char*>(a.dout + b * a.do_sb + head * a.do_sh + (int64_t)pos * a.do_sl);
-#pragma unroll
-    for (int s = 0; s < T::SSTEPS; s++) {
-      i32x4 zero = {0, 0, 0, 0}, qr = zero, dr = zero, orow = zero;
-      if (counts) {   // (rows that do not count may hold anything)
-        qr = *reinterpret_cast<const i32x4*>(qp + (2 * s + g) * 16);
-        dr = *reinterpret_cast<const i32x4*>(dp + (2 * s + g) * 16);
-        orow = *reinterpret_cast<const i32x4*>(op + (2 * s + g) * 16);
-      }
-      qf[s] = __builtin_bit_cast(bf16x8, qr);
-      dof[s] = __builtin_bit_cast(bf16x8, dr);
-      const bf16x8 of = __builtin_bit_cast(bf16x8, orow);
-#pragma unroll
-      for (int e = 0; e < 8; e++) delta += (float)of[e] * (float)dof[s][e];
-    }
-  }
-  delta = lane_pair_sum(delta);
-  const int64_t at = ((int64_t)b * a.H + head) * a.Lq + pos;
-  const float lse2 = counts ? a.lse[at] * 1.44269504088896340736f : INFINITY;
-  if (counts && g == 0) {
-    const f32x2 st = {lse2, delta};
-    *reinterpret_cast<f32x2*>(a.stats + 2 * at) = st;
-  }
-
-  f32x16 acc[T::DBLK];
-#pragma unroll
-  for (int db = 0; db < T::DBLK; db++)
-#pragma unroll
-    for (int r = 0; r < 16; r++) acc[db][r] = 0.0f;
-  const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh;
-  const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh;
-  const unsigned k_rowb = (unsigned)(a.k_sl * 2), v_rowb = (unsigned)(a.v_sl * 2);
   const unsigned lds0 = lds_address(smem);
   TileReader<D> rd;
   rd.place(lane);
-  const int ntiles = (k_len + 31) / 32;
-  auto fetch = [&](int t) {
-    const unsigned slot = lds0 + (t & 1) * 2 * T::BYTES;
-    fetch_rows<D, 8>(kbase, k_rowb, t * 32, k_len - 1, wv * 8, slot, lane);
-    fetch_rows<D, 8>(vbase, v_rowb, t * 32, k_len - 1, wv * 8, slot + T::BYTES, lane);
-  };
-  if (ntiles > 0) fetch(0);
-  for (int t = 0; t < ntiles; t++) {
+  const int lrow = lane / T::CH, pc = lane % T::CH;
+
+  // workgroups of one XCD take neighbouring ranges of units
+  const int G = gridDim.x, per = G >> 3, rem = G & 7, x = blockIdx.x & 7;
+  const int64_t me = x * per + min(x, rem) + (blockIdx.x >> 3);
+  int at_unit = (int)(a.dq_units * me / G);
+  const int end_unit = (int)(a.dq_units * (me + 1) / G);
+  const unsigned k_rowb = (unsigned)(a.k_sl * 2), v_rowb = (unsigned)(a.v_sl * 2);
+
+  f32x16 acc[DBLK], SA, SB, DA, DB;
+  bf16x8 qf[NE], dof[NE];
+  bool again = false;
+  while (at_unit < end_unit) {   // one range of one key head's keys
+    const int part = at_unit / a.QU, first_unit = at_unit - part * a.QU, first = first_unit * a.unit;
+    const int slice = part / a.k_split, split = part - slice * a.k_split;
+    const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
+    const int n_here = min(a.QU - first_unit, end_unit - at_unit);
+    at_unit += n_here;
+    const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
+    const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+    const int key0 = split * a.split_keys, cnt = max(0, min(k_len - key0, a.split_keys));
+    const int np = (cnt + 63) >> 6;
+    const int last = min(first + n_here * a.unit, a.QB);
+    const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh + key0 * a.k_sl;
+    const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh + key0 * a.v_sl;
+    if (again) __syncthreads();   // every wave is done with the keys before
+    again = true;
+    // Rows r .. of pair `pair` of K or V -> LDS.  Rows past the last key are read as the last one: finite wherever the tensor is, and
+    // multiplied by zero.
+    auto fetch = [&](const uint16_t* base, unsigned row_bytes, int pair, int r, unsigned at) {
+      const int key = min(pair * 64 + r + lrow, cnt - 1);
+      gather16(base, __umul24((unsigned)key, row_bytes) + (unsigned)((pc ^ T::swz((r + lrow) & 31)) << 4), at + r * T::ROWB);
+    };
+    int next = 0, next_slot = 0;   // STREAM: the pair that is fetched next and the slot it goes to
+    auto fetch_kv = [&](int i) {   // load i of 2 IPW of this wave
+      const int r = (wv * IPW + (i < IPW ? i : i - IPW)) * RPI;
+      if (i < IPW) fetch(kbase, k_rowb, next, r, lds0 + next_slot * 2 * PB2);
+      else fetch(vbase, v_rowb, next, r, lds0 + next_slot * 2 * PB2 + PB2);
+      if (i + 1 < 2 * IPW) return;
+      next = next + 1 == np ? 0 : next + 1;
+      next_slot = next_slot + 1 == SLOTS ? 0 : next_slot + 1;
+    };
+    if constexpr (STREAM) {
+      if (np > 0)
+        for (int n = 0; n + 1 < SLOTS; n++)
+          for (int i = 0; i < 2 * IPW; i++) fetch_kv(i);
+    } else {
+      for (int i = wv; i < np * (64 / RPI); i += WV) {
+        const int pair = i / (64 / RPI), r = (i - pair * (64 / RPI)) * RPI;
+        fetch(kbase, k_rowb, pair, r, lds0 + pair * 2 * PB2);
+        fetch(vbase, v_rowb, pair, r, lds0 + pair * 2 * PB2 + PB2);
+      }
+    }
     wait_vmem_all();
-    __syncthreads();   // tile t is there, and every wave is done with the slot of tile t + 1
-    if (t + 1 < ntiles) fetch(t + 1);
-    const unsigned char* kt = smem + (t & 1) * 2 * T::BYTES;
-    const unsigned char* vt = kt + T::BYTES;
-    f32x16 S, dP;
+    __syncthreads();
+
+    int slot = 0;   // STREAM: of the pair whose dS comes next
+    const int turns = (last - first + WV - 1) / WV;
+    for (int turn = 0; turn < turns; turn++) {
+      const int j = first + turn * WV + wv;
+      if (!STREAM && j >= last) break;   // (STREAM: a wave without a tile goes through the keys along with the others)
+      // this lane's row (worked out again where it is stored: no registers for it in between)
+      int pos, head;
+      bool mine, counts;
+      auto place = [&](int j) {
+        int of_tile = ln;
+        asm volatile("" : "+v"(of_tile));
+        const int my_row = j * 32 + of_tile, row = min(my_row, a.rows - 1);
+        const int of_group = a.group > 1 ? (int)((unsigned)row / (unsigned)a.Lq) : 0;
+        pos = row - of_group * a.Lq;
+        head = hk * a.group + of_group;
+        mine = j < last && my_row < a.rows;
+        counts = mine && pos < q_len && k_len > 0;
+        return ((int64_t)b * a.H + head) * a.Lq + pos;
+      };
+      const int64_t at = place(j);
+      float delta = 0.0f;
+      {
+        const char* qp = reinterpret_cast<const char*>(a.q + b * a.q_sb + head * a.q_sh + (int64_t)pos * a.q_sl);
+        const char* op = reinterpret_cast<const char*>(a.o + b * a.o_sb + head * a.o_sh + (int64_t)pos * a.o_sl);
+        const char* dp = reinterpret_cast<const char*>(a.dout + b * a.do_sb + head * a.do_sh + (int64_t)pos * a.do_sl);
+        i32x4 orow[NE];
 #pragma unroll
-    for (int r = 0; r < 16; r++) S[r] = dP[r] = 0.0f;
+        for (int s = 0; s < NE; s++) {
+          i32x4 zero = {0, 0, 0, 0}, qr = zero, dr = zero;
+          orow[s] = zero;
+          if (counts) {   // (rows that do not count may hold anything)
+            qr = *reinterpret_cast<const i32x4*>(qp + (2 * s + g) * 16);
+            dr = *reinterpret_cast<const i32x4*>(dp + (2 * s + g) * 16);
+            if (!a.own_delta) orow[s] = *reinterpret_cast<const i32x4*>(op + (2 * s + g) * 16);
+          }
+          qf[s] = __builtin_bit_cast(bf16x8, qr);
+          dof[s] = __builtin_bit_cast(bf16x8, dr);
+        }
 #pragma unroll
-    for (int s = 0; s < T::SSTEPS; s++) {
-      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.rows(kt, s), qf[s], S, 0, 0, 0);
-      dP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.rows(vt, s), dof[s], dP, 0, 0, 0);
+        for (int s = 0; s < NE; s++) {
+          const bf16x8 of = __builtin_bit_cast(bf16x8, orow[s]);
+#pragma unroll
+          for (int e = 0; e < 8; e++) delta += (float)of[e] * (float)dof[s][e];
+        }
+      }
+      delta = lane_pair_sum(delta);
+      const float lse2 = counts ? a.lse[at] * 1.44269504088896340736f : INFINITY;
+      constexpr int AHEAD = 2;
+      // Sn, dPn of the tile at k_at (its V 64 rows further on)
+      auto scores = [&](int k_at, f32x16& Sn, f32x16& dPn, auto between) {
+        int kb = rd.row_off + k_at;
+        asm volatile("" : "+v"(kb));   // (one addition here, and plain XORs with constants below)
+        bf16x8 kf[NE], vf[NE];
+        auto read = [&](int s) {
+          kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + (kb ^ (32 * s))));
+          vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + PB2 + (kb ^ (32 * s))));
+        };
+#pragma unroll
+        for (int s = 0; s < AHEAD; s++) read(s);
+#pragma unroll
+        for (int r = 0; r < 16; r++) Sn[r] = dPn[r] = 0.0f;
+        auto one = [&](auto sc) {
+          constexpr int s = decltype(sc)::value;
+          if constexpr (s + AHEAD < NE) read(s + AHEAD);
+          Sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], Sn, 0, 0, 0);
+          dPn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s], dof[s], dPn, 0, 0, 0);
+          between(sc);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        [&]<int... E>(std::integer_sequence<int, E...>) { (one(std::integral_constant<int, E>()), ...); }(std::make_integer_sequence<int, NE>());
+      };
+      i32x4 ds[2];
+      // dS of tile t out of So, dPo; the elements of slot e
+      auto form = [&](auto ec, const f32x16& So, const f32x16& dPo) {
+        constexpr int e = decltype(ec)::value, VPS = 16 / NE;
+#pragma unroll
+        for (int y = 0; y < VPS; y += 2) {
+          const int r = e * VPS + y;
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r], a.c_log2, -lse2));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r + 1], a.c_log2, -lse2));
+          const f32x2 dd = {p0 * (dPo[r] - delta), p1 * (dPo[r + 1] - delta)};
+          int pk = __builtin_bit_cast(int, __builtin_convertvector(dd, bf16x2));
+          asm volatile("" : "+v"(pk));   // keeps the compiler from sinking the conversion out of the slot
+          ds[r >> 3][(r & 7) >> 1] = pk;
+        }
+      };
+      // keys of tile t that do not count: dS = 0 (element 2 i of the packed pairs is the key of register 2 i)
+      auto mask = [&](int t) {
+        const int limit = cnt - 32 * t;
+        if (__builtin_expect(limit < 32, 0)) {
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const int key = 8 * (r >> 2) + 4 * g + (r & 3);
+            ds[r >> 3][(r & 7) >> 1] &= (key < limit ? 0xFFFF : 0) | (key + 1 < limit ? (int)0xFFFF0000 : 0);
+          }
+        }
+      };
+      auto add = [&](int k_at) {   // dQ^T += K^T dS^T
+        const bf16x8 d2[2] = {__builtin_bit_cast(bf16x8, ds[0]), __builtin_bit_cast(bf16x8, ds[1])};
+#pragma unroll
+        for (int db = 0; db < DBLK; db++)
+#pragma unroll
+          for (int c = 0; c < 2; c++)
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.transposed(smem + k_at, db, c), d2[c], acc[db], 0, 0, 0);
+      };
+      if (!STREAM && a.own_delta) {   // D = sum over the keys of P dP
+        auto sum = [&](int t, const f32x16& So, const f32x16& dPo) {
+          const int limit = cnt - 32 * t - 4 * g;
+#pragma unroll
+          for (int r = 0; r < 16; r++) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(So[r], a.c_log2, -lse2));
+            delta += 8 * (r >> 2) + (r & 3) < limit ? p * dPo[r] : 0.0f;
+          }
+        };
+        for (int p = 0; p < np; p++) {
+          scores(p * 2 * PB2, SA, DA, [](auto) {});
+          scores(p * 2 * PB2 + TB, SB, DB, [&](auto ec) {
+            if constexpr (decltype(ec)::value == 0) sum(2 * p, SA, DA);
+          });
+          sum(2 * p + 1, SB, DB);
+        }
+        delta = lane_pair_sum(delta);
+      }
+      if (counts && g == 0 && split == 0) {
+        const f32x2 st = {lse2, delta};
+        *reinterpret_cast<f32x2*>(a.stats + 2 * at) = st;
+      }
+#pragma unroll
+      for (int db = 0; db < DBLK; db++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc[db][r] = 0.0f;
+      if (np > 0) {
+        int k_at = STREAM ? slot * 2 * PB2 : 0;
+        scores(k_at, SA, DA, [](auto) {});
+        for (int p = 0; p < np; p++) {
+          int k_next = k_at + 2 * PB2;
+          if constexpr (STREAM) {
+            // pair p + 1 has arrived, and every wave is done with pair p - 1: the pair SLOTS - 1 ahead follows into its slot
+            wait_vmem_le<(SLOTS - 3) * 2 * IPW>();
+            __syncthreads();
+            slot = slot + 1 == SLOTS ? 0 : slot + 1;
+            k_next = slot * 2 * PB2;
+          }
+          // tile 2 p + 1 beside tile 2 p
+          scores(k_at + TB, SB, DB, [&](auto ec) {
+            form(ec, SA, DA);
+            if constexpr (STREAM && decltype(ec)::value % (NE / 2) == 1 && decltype(ec)::value / (NE / 2) < IPW) fetch_kv(decltype(ec)::value / (NE / 2));
+          });
+          mask(2 * p);
+          add(k_at);
+          // the next pair's first tile beside tile 2 p + 1
+          auto second = [&](auto ec) {
+            form(ec, SB, DB);
+            if constexpr (STREAM && decltype(ec)::value % (NE / 2) == 1 && decltype(ec)::value / (NE / 2) < IPW) fetch_kv(IPW + decltype(ec)::value / (NE / 2));
+          };
+          if (p + 1 < np) scores(k_next, SA, DA, second);
+          else [&]<int... E>(std::integer_sequence<int, E...>) { (second(std::integral_constant<int, E>()), ...); }(std::make_integer_sequence<int, NE>());
+          mask(2 * p + 1);
+          add(k_at + TB);
+          k_at = k_next;
+        }
+      }
+      const int64_t to = place(j);
+      if (a.k_split > 1) {
+        if (mine) {
+          float* dst = a.part_q + ((int64_t)split * a.B * a.H * a.Lq + to) * D;
+#pragma unroll
+          for (int db = 0; db < DBLK; db++)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; r4++)
+              *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * r4 + 4 * g) = f32x4{acc[db][4 * r4], acc[db][4 * r4 + 1], acc[db][4 * r4 + 2], acc[db][4 * r4 + 3]};
+        }
+      } else {   // (zeros where the row does not count)
+        store_row16<D>(a.dq + b * a.dq_sb + head * a.dq_sh + (int64_t)pos * a.dq_sl, acc, counts ? a.scale : 0.0f, g, mine);
+      }
     }
-    f32x16 dS;
-#pragma unroll
-    for (int r = 0; r < 16; r++) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], a.c_log2, -lse2));
-      dS[r] = p * (dP[r] - delta);
-    }
-    if (t * 32 + 32 > k_len) {
-#pragma unroll
-      for (int r = 0; r < 16; r++)
-        if (t * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= k_len) dS[r] = 0.0f;
-    }
-    bf16x8 ds[2];
-    pack_rows(dS, ds);
-#pragma unroll
-    for (int db = 0; db < T::DBLK; db++)
-#pragma unroll
-      for (int c = 0; c < 2; c++)
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.transposed(kt, db, c), ds[c], acc[db], 0, 0, 0);
+    if constexpr (STREAM) wait_vmem_all();   // (pairs that nobody reads; none may land after this workgroup)
   }
-  if (my_row < rows)   // (zeros where the row does not count)
-    store_row<D>(a.dq + b * a.dq_sb + head * a.dq_sh + (int64_t)pos * a.dq_sl, acc, counts ? a.scale : 0.0f, g);
 }
 
 template <int D>
@@ -359,6 +516,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs a) {
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
   if (key < k_len && q_len > 0) {
     const float* src = a.part + row * 2 * D + e;
+#pragma unroll 8
     for (int s = 0; s < a.n_split; s++) sum += *reinterpret_cast<const f32x4*>(src + s * n_rows * 2 * D);
   }
   uint16_t* dst;
@@ -371,15 +529,36 @@ __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs a) {
   *reinterpret_cast<i32x2*>(dst) = __builtin_bit_cast(i32x2, __builtin_convertvector(sum, bf16x4));
 }
 
+// dQ of split keys: a thread adds up four elements of one row over the ranges, in order.
+template <int D>
+__global__ void __launch_bounds__(256) sum_q_kernel(const BwdArgs a) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / (D / 4), n_rows = (int64_t)a.B * a.H * a.Lq;
+  const int e = (int)(t - row * (D / 4)) * 4;
+  if (row >= n_rows) return;
+  const int l = (int)(row % a.Lq), bh = (int)(row / a.Lq), b = bh / a.H, h = bh - b * a.H;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (!a.q_lens || l < a.q_lens[b]) {
+    const float* src = a.part_q + row * D + e;
+#pragma unroll 8
+    for (int s = 0; s < a.k_split; s++) sum += *reinterpret_cast<const f32x4*>(src + s * n_rows * D);
+    sum *= a.scale;
+  }
+  *reinterpret_cast<i32x2*>(a.dq + b * a.dq_sb + h * a.dq_sh + (int64_t)l * a.dq_sl + e) =
+      __builtin_bit_cast(i32x2, __builtin_convertvector(sum, bf16x4));
+}
+
+constexpr int kOwnDelta = 128;   // see the top of the file
+
 struct BwdPlan {
-  int QB, KB, units, n_split, units_per_split;
-  size_t stats_bytes, bytes;
+  int KB, units, n_split, units_per_split;                      // dkdv_kernel
+  int QB, unit, QU, k_split, split_keys;                        // dq_kernel
+  bool stream;
+  size_t stats_bytes, part_bytes, part_q_bytes, bytes;
 };
-static BwdPlan bwd_plan(const fgattn_cross_params* p) {
+static BwdPlan bwd_plan(const fgattn_cross_params* p, int cus) {
   BwdPlan s;
   const int64_t slices = (int64_t)p->B * p->Hkv;
   const int group = p->H / p->Hkv;
-  s.QB = (int)(((int64_t)group * p->Lq + 127) / 128);
   s.KB = (p->Lk + 127) / 128;
   s.units = group * ((p->Lq + 31) / 32);
   const int64_t tiles = slices * s.KB;
@@ -387,34 +566,65 @@ static BwdPlan bwd_plan(const fgattn_cross_params* p) {
   if (n > s.units) n = s.units;
   s.units_per_split = (int)((s.units + n - 1) / n);
   s.n_split = (s.units + s.units_per_split - 1) / s.units_per_split;
-  s.stats_bytes = ((size_t)p->B * p->H * p->Lq * 2 * sizeof(float) + 255) & ~(size_t)255;
-  s.bytes = s.stats_bytes;
-  if (s.n_split > 1) s.bytes += ((size_t)s.n_split * slices * p->Lk * 2 * p->d * sizeof(float) + 255) & ~(size_t)255;
+
+  s.QB = (int)(((int64_t)group * p->Lq + 31) / 32);
+  const int64_t q_tiles = slices * s.QB;
+  const int fit = kLdsBytes / (4 * p->d) / 64 * 64;             // keys that LDS holds
+  s.stream = p->Lk > fit && q_tiles * q_tiles * p->d >= 9000 * (int64_t)p->Lk;
+  s.k_split = 1;
+  s.split_keys = p->Lk;
+  if (p->Lk > fit && !s.stream) {
+    int64_t ranges = (2048 + q_tiles - 1) / q_tiles;
+    const int64_t least = (p->Lk + fit - 1) / fit, most = (p->Lk + 127) / 128;
+    ranges = ranges < least ? least : ranges > most ? most : ranges;
+    s.split_keys = (int)((p->Lk + ranges - 1) / ranges + 63) / 64 * 64;
+    s.k_split = (p->Lk + s.split_keys - 1) / s.split_keys;
+  }
+  s.unit = s.stream ? 8 : 1;
+  const int64_t groups = cus / (slices * s.k_split);
+  if (groups >= 1 && (s.QB + groups - 1) / groups <= 8) s.unit = (int)((s.QB + groups - 1) / groups);
+  s.QU = (s.QB + s.unit - 1) / s.unit;
+  auto round = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  s.stats_bytes = round((size_t)p->B * p->H * p->Lq * 2 * sizeof(float));
+  s.part_bytes = s.n_split > 1 ? round((size_t)s.n_split * slices * p->Lk * 2 * p->d * sizeof(float)) : 0;
+  s.part_q_bytes = s.k_split > 1 ? round((size_t)s.k_split * p->B * p->H * p->Lq * p->d * sizeof(float)) : 0;
+  s.bytes = s.stats_bytes + s.part_bytes + s.part_q_bytes;
   return s;
 }
 
-template <int D>
-static int launch_bwd(BwdArgs& a, const BwdPlan& s, hipStream_t stream) {
+template <typename Kernel>
+static int launch_lds(Kernel kernel, int most, int lds, dim3 grid, int threads, hipStream_t stream, const BwdArgs& a, bool (&ready)[64]) {
   static std::mutex mutex;
-  static bool ready[64];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return FGATTN_E_DEVICE;
   {
     std::lock_guard<std::mutex> lock(mutex);
     if (!ready[dev]) {
-      if (hipFuncSetAttribute(reinterpret_cast<const void*>(dkdv_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                              dkdv_lds_bytes<D>()) != hipSuccess)
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess)
         return FGATTN_E_DEVICE;
       ready[dev] = true;
     }
   }
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, stream, a);
+  return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;
+}
+
+template <int D>
+static int launch_bwd(BwdArgs& a, const BwdPlan& s, int cus, hipStream_t stream) {
+  static bool ready[3][64];
   const int slices = a.B * a.Hkv;
-  a.n_items = slices * s.QB;
-  hipLaunchKernelGGL(dq_kernel<D>, dim3(a.n_items), dim3(256), 0, stream, a);
-  if (hipGetLastError() != hipSuccess) return FGATTN_E_DEVICE;
+  const dim3 dq_grid(a.dq_units < cus ? a.dq_units : cus);
+  int rc = s.stream ? launch_lds(dq_kernel<D, true>, kLdsBytes, kLdsBytes, dq_grid, 512, stream, a, ready[0])
+                    : launch_lds(dq_kernel<D, false>, kLdsBytes, (s.split_keys + 63) / 64 * 64 * 4 * D, dq_grid, 512, stream, a, ready[1]);
+  if (rc) return rc;
+  if (s.k_split > 1) {
+    const int64_t threads = (int64_t)a.B * a.H * a.Lq * (D / 4);
+    hipLaunchKernelGGL(sum_q_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
+    if (hipGetLastError() != hipSuccess) return FGATTN_E_DEVICE;
+  }
   a.n_items = slices * s.KB * s.n_split;
-  hipLaunchKernelGGL(dkdv_kernel<D>, dim3(a.n_items), dim3(256), dkdv_lds_bytes<D>(), stream, a);
-  if (hipGetLastError() != hipSuccess) return FGATTN_E_DEVICE;
+  rc = launch_lds(dkdv_kernel<D>, dkdv_lds_bytes<D>(), dkdv_lds_bytes<D>(), dim3(a.n_items), 256, stream, a, ready[2]);
+  if (rc) return rc;
   if (s.n_split > 1) {
     const int64_t threads = (int64_t)slices * a.Lk * (2 * D / 4);
     hipLaunchKernelGGL(sum_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, a);
@@ -428,7 +638,7 @@ static int launch_bwd(BwdArgs& a, const BwdPlan& s, hipStream_t stream) {
 extern "C" {
 
 size_t fgattn_cross_backward_workspace_bytes(const fgattn_cross_params* p) {
-  return fgx::check_shape(p) == FGATTN_OK ? fgx::bwd_plan(p).bytes : 0;
+  return fgx::check_shape(p) == FGATTN_OK ? fgx::bwd_plan(p, 1).bytes : 0;   // (how many compute units there are does not matter to the sizes)
 }
 
 int fgattn_cross_backward(const void* q, const void* k, const void* v, const void* out, const float* lse, const void* dout,
@@ -447,9 +657,10 @@ int fgattn_cross_backward(const void* q, const void* k, const void* v, const voi
   if ((rc = fgx::check_tensor(dv, p->dv_stride_b, p->dv_stride_h, p->dv_stride_l, p->B, p->Hkv, p->Lk, p->d, false, true))) return rc;
   if ((reinterpret_cast<uintptr_t>(lse) & 3) != 0) return FGATTN_E_ALIGN;
   if ((rc = fgx::check_lens(q_lens, k_lens))) return rc;
-  const fgx::BwdPlan s = fgx::bwd_plan(p);
-  if ((rc = fgx::check_workspace(workspace, workspace_bytes, s.bytes))) return rc;
-  if ((rc = fg::require_device(nullptr))) return rc;
+  if ((rc = fgx::check_workspace(workspace, workspace_bytes, fgattn_cross_backward_workspace_bytes(p)))) return rc;
+  int cus = 0;
+  if ((rc = fg::require_device(&cus))) return rc;
+  const fgx::BwdPlan s = fgx::bwd_plan(p, cus);
   fgx::BwdArgs a = {};
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -464,6 +675,7 @@ int fgattn_cross_backward(const void* q, const void* k, const void* v, const voi
   a.k_lens = k_lens;
   a.stats = static_cast<float*>(workspace);
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + s.stats_bytes);
+  a.part_q = reinterpret_cast<float*>(static_cast<char*>(workspace) + s.stats_bytes + s.part_bytes);
   a.q_sb = p->q_stride_b; a.q_sh = p->q_stride_h; a.q_sl = p->q_stride_l;
   a.k_sb = p->k_stride_b; a.k_sh = p->k_stride_h; a.k_sl = p->k_stride_l;
   a.v_sb = p->v_stride_b; a.v_sh = p->v_stride_h; a.v_sl = p->v_stride_l;
@@ -473,11 +685,14 @@ int fgattn_cross_backward(const void* q, const void* k, const void* v, const voi
   a.dk_sb = p->dk_stride_b; a.dk_sh = p->dk_stride_h; a.dk_sl = p->dk_stride_l;
   a.dv_sb = p->dv_stride_b; a.dv_sh = p->dv_stride_h; a.dv_sl = p->dv_stride_l;
   a.B = p->B; a.H = p->H; a.Hkv = p->Hkv; a.group = p->H / p->Hkv; a.Lq = p->Lq; a.Lk = p->Lk;
-  a.QB = s.QB; a.KB = s.KB; a.n_split = s.n_split; a.units = s.units; a.units_per_split = s.units_per_split;
+  a.rows = a.group * p->Lq; a.QB = s.QB; a.unit = s.unit; a.QU = s.QU; a.dq_units = p->B * p->Hkv * s.k_split * s.QU;
+  a.k_split = s.k_split; a.split_keys = s.split_keys;
+  a.own_delta = p->Lk <= fgx::kOwnDelta;
+  a.KB = s.KB; a.n_split = s.n_split; a.units = s.units; a.units_per_split = s.units_per_split;
   a.scale = p->scale;
   a.c_log2 = p->scale * 1.44269504088896340736f;
-  return p->d == 64 ? fgx::launch_bwd<64>(a, s, static_cast<hipStream_t>(stream))
-                    : fgx::launch_bwd<128>(a, s, static_cast<hipStream_t>(stream));
+  return p->d == 64 ? fgx::launch_bwd<64>(a, s, cus, static_cast<hipStream_t>(stream))
+                    : fgx::launch_bwd<128>(a, s, cus, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

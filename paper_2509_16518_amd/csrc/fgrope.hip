@@ -22,7 +22,7 @@ namespace fgr {
 // fp32 rounding as the only one that shows.  A wave's lanes are neighbouring pairs: every store is a run of whole lines.
 // ------------------------------------------------------------------------------------------
 struct Axis {
-  double log_theta, offset, step, factor, original, beta_fast, beta_slow;
+  double log_speed, offset, step, slower, turns, beta_slow, per_beta;   // pair j: speed e^(j log_speed), trained turns `turns` times that
   int32_t size, pairs, first, inner;   // first pair's column; rows per step of the coordinate
 };
 struct TableArgs {
@@ -34,23 +34,18 @@ struct TableArgs {
 };
 
 __global__ void __launch_bounds__(256) table_kernel(const TableArgs a) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t group = t / a.pairs;
+  const unsigned t = blockIdx.x * 256 + threadIdx.x;   // (at most 2^20 runs of 128 pairs)
+  const unsigned group = t / (unsigned)a.pairs;
   const int col = (int)(t - group * a.pairs);
-  const int64_t first_row = group * a.run;
-  if (first_row >= a.rows) return;
-  const int row0 = (int)first_row, row1 = (int)(first_row + a.run < a.rows ? first_row + a.run : a.rows);
+  const int row0 = (int)group * a.run, row1 = min(row0 + a.run, a.rows);
+  if (row0 >= a.rows) return;
   Axis x = a.axis[0];
   if (a.n_axes > 1 && col >= a.axis[1].first) x = a.axis[1];
   if (a.n_axes > 2 && col >= a.axis[2].first) x = a.axis[2];
-  const double w = exp(-x.log_theta * (double)(col - x.first) / (double)x.pairs);
-  double kept = 0.0;
-  if (x.original > 0.0) {
-    const double turns = x.original * w * 0.15915494309189533577;
-    kept = (turns - x.beta_slow) / (x.beta_fast - x.beta_slow);
-    kept = kept < 0.0 ? 0.0 : kept > 1.0 ? 1.0 : kept;
-  }
-  const double speed = w * (kept + (1.0 - kept) / x.factor);
+  const double w = exp(x.log_speed * (double)(col - x.first));
+  double kept = (x.turns * w - x.beta_slow) * x.per_beta;
+  kept = kept < 0.0 ? 0.0 : kept > 1.0 ? 1.0 : kept;
+  const double speed = w * (kept + (1.0 - kept) * x.slower);
   int coord = (row0 / x.inner) % x.size;
   int left = x.inner - row0 % x.inner;   // rows until the coordinate moves
   double c, s, dc = 1.0, ds = 0.0;
@@ -140,6 +135,32 @@ struct RowLane {
     const bool turns = (unsigned)row < (unsigned)a.table_rows;
     const int half = a.rot >> 1;
     const int64_t at = (int64_t)(turns ? row : 0) * half;
+    // a chunk whose pairs are neighbours and all turn: whole loads (of any alignment)
+    if constexpr (PAIRS != PAIRS_HALF_ODD) {
+      constexpr int N = PAIRS == PAIRS_NEXT ? V / 2 : V;
+      typedef float Pairs __attribute__((ext_vector_type(N), aligned(4)));
+      if (PAIRS == PAIRS_HALF || e0 + V <= a.rot) {
+        const int pair = PAIRS == PAIRS_NEXT ? e0 >> 1 : e0 < half ? e0 : e0 < a.rot ? e0 - half : 0;
+        const bool on = turns && e0 < a.rot;
+        Pairs cs, sn;
+        for (int i = 0; i < N; i++) {
+          cs[i] = 1.0f;
+          sn[i] = 0.0f;
+        }
+        if (on) {
+          cs = *reinterpret_cast<const Pairs*>(a.cos + at + pair);
+          sn = *reinterpret_cast<const Pairs*>(a.sin + at + pair);
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+          const bool first = PAIRS == PAIRS_NEXT ? (i & 1) == 0 : e0 < half;
+          c[i] = cs[PAIRS == PAIRS_NEXT ? i >> 1 : i];
+          const float s1 = sn[PAIRS == PAIRS_NEXT ? i >> 1 : i];
+          s[i] = first != back ? -s1 : s1;
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < V; i++) {
       const int e = e0 + i;
@@ -167,18 +188,33 @@ struct RowLane {
     }
     return r;
   }
-  __device__ __forceinline__ void weights(const RopeArgs& a, int t, float (&w)[V], float (&wp)[V]) const {
-    const int half = a.rot >> 1;
+  // weights of the lane's elements and of their partners
+  template <typename W>
+  __device__ __forceinline__ void load_weights(const RopeArgs& a, const W* from, float (&w)[V], float (&wp)[V]) const {
+    typedef W Some __attribute__((ext_vector_type(V), aligned(sizeof(W))));   // (of any alignment)
+    const Some own = *reinterpret_cast<const Some*>(from + e0);
+    Some far = own;
+    if constexpr (PAIRS == PAIRS_HALF) far = *reinterpret_cast<const Some*>(from + other);
+    if constexpr (PAIRS == PAIRS_HALF_ODD) {
+      const int half = a.rot >> 1;
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-      const int e = e0 + i;
-      const int p = PAIRS == PAIRS_NEXT ? (e ^ 1) : e < half ? e + half : e < a.rot ? e - half : e;
-      w[i] = wp[i] = 1.0f;
-      if (a.w[t] != nullptr) {
-        w[i] = a.w_fp32 ? static_cast<const float*>(a.w[t])[e] : (float)static_cast<const T*>(a.w[t])[e];
-        wp[i] = a.w_fp32 ? static_cast<const float*>(a.w[t])[p] : (float)static_cast<const T*>(a.w[t])[p];
+      for (int i = 0; i < V; i++) {
+        const int e = e0 + i;
+        far[i] = from[e < half ? e + half : e < a.rot ? e - half : e];
       }
     }
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+      w[i] = (float)own[i];
+      wp[i] = (float)far[PAIRS == PAIRS_NEXT ? i ^ 1 : i];
+    }
+  }
+  __device__ __forceinline__ void weights(const RopeArgs& a, int t, float (&w)[V], float (&wp)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; i++) w[i] = wp[i] = 1.0f;
+    if (a.w[t] == nullptr) return;
+    if (a.w_fp32) load_weights(a, static_cast<const float*>(a.w[t]), w, wp);
+    else load_weights(a, static_cast<const T*>(a.w[t]), w, wp);
   }
 };
 
@@ -330,6 +366,7 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial,
   const int e = threadIdx.x & 15, slice = threadIdx.x >> 4, at = blockIdx.x * 16 + e;
   float sum = 0.0f;
   if (at < d)
+#pragma unroll 8
     for (int g = slice; g < groups; g += 64) sum += partial[((int64_t)g * 2 + blockIdx.y) * d + at];
   sums[slice][e] = sum;
   __syncthreads();
@@ -502,9 +539,15 @@ int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, float mscale, fl
       return FGATTN_E_SCALE;
     if (x.original > 0.0 && (!isfinite(x.beta_fast) || !isfinite(x.beta_slow) || !(x.beta_fast > x.beta_slow))) return FGATTN_E_SCALE;
     fgr::Axis& y = a.axis[n];
-    y.log_theta = ::log(x.theta);
-    y.offset = x.offset; y.step = x.step; y.factor = x.factor; y.original = x.original;
-    y.beta_fast = x.beta_fast; y.beta_slow = x.beta_slow;
+    y.log_speed = -::log(x.theta) / x.pairs;
+    y.offset = x.offset;
+    y.step = x.step;
+    y.slower = 1.0 / x.factor;
+    if (x.original > 0.0) {   // (otherwise nothing is kept: 0 turns over the trained length)
+      y.turns = x.original * 0.15915494309189533577;
+      y.beta_slow = x.beta_slow;
+      y.per_beta = 1.0 / (x.beta_fast - x.beta_slow);
+    }
     y.size = x.size; y.pairs = x.pairs; y.first = (int32_t)pairs;
     rows *= x.size;
     pairs += x.pairs;
@@ -517,7 +560,9 @@ int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, float mscale, fl
   if (rc) return rc;
   a.cos = cos; a.sin = sin;
   a.n_axes = n_axes; a.rows = (int32_t)rows; a.pairs = (int32_t)pairs; a.mscale = mscale;
-  a.run = 16;
+  // Rows of a thread: more spread the cost of its first sines and cosines, fewer fill the chip.  32760 rows of 64 pairs: 8 rows 10.1 us,
+  // 16 8.7, 32 9.4, 64 11.5; 118800 rows: 21.9, 18.2, 15.6, 15.7.
+  a.run = rows * pairs >= (4 << 20) ? 32 : 16;
   const int64_t threads = ((rows + a.run - 1) / a.run) * pairs;
   hipLaunchKernelGGL(fgr::table_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;
