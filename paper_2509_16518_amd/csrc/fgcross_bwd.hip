@@ -562,24 +562,32 @@ static BwdPlan bwd_plan(const fgattn_cross_params* p, int cus) {
   s.KB = (p->Lk + 127) / 128;
   s.units = group * ((p->Lq + 31) / 32);
   const int64_t tiles = slices * s.KB;
-  int64_t n = tiles < 512 ? 512 / tiles : 1;
+  // Ranges of rows: two workgroups for each of 256 compute units, but one where that leaves a workgroup less than 16 tiles of rows to
+  // read for the K and V that it waits for and the sums that it writes (the whole call, one against two: 12 x 32760 tokens to
+  // 512 keys 451 and 422 us, 12 x 1000 tokens to 512 keys 48 and 53, 2 x 8 x 2635 tokens to 77 keys of d = 64 28 and 31).
+  int64_t n = 512 / tiles;
+  const int64_t one = 256 / tiles, by_rows = s.units / 16;
+  if (n > one && n > by_rows) n = one > by_rows ? one : by_rows;
   if (n > s.units) n = s.units;
+  if (n < 1) n = 1;
   s.units_per_split = (int)((s.units + n - 1) / n);
   s.n_split = (s.units + s.units_per_split - 1) / s.units_per_split;
 
   s.QB = (int)(((int64_t)group * p->Lq + 31) / 32);
-  const int64_t q_tiles = slices * s.QB;
   const int fit = kLdsBytes / (4 * p->d) / 64 * 64;             // keys that LDS holds
-  s.stream = p->Lk > fit && q_tiles * q_tiles * p->d >= 9000 * (int64_t)p->Lk;
   s.k_split = 1;
   s.split_keys = p->Lk;
-  if (p->Lk > fit && !s.stream) {
-    int64_t ranges = (2048 + q_tiles - 1) / q_tiles;
-    const int64_t least = (p->Lk + fit - 1) / fit, most = (p->Lk + 127) / 128;
-    ranges = ranges < least ? least : ranges > most ? most : ranges;
-    s.split_keys = (int)((p->Lk + ranges - 1) / ranges + 63) / 64 * 64;
+  if (p->Lk > fit) {
+    // as many ranges as make a workgroup of eight tiles for each of 256 compute units, of 128 keys or more; their partial sums stay
+    // below 256 x 8 tiles, 34 MB (64 tokens of 8 heads, 8192 keys: the whole call 253 us in one range, 41 in 32; 24 x 1000
+    // tokens, 2048 keys 134 and 125)
+    int64_t ranges = 256 / (slices * ((s.QB + 7) / 8));
+    const int64_t most = (p->Lk + 127) / 128;
+    ranges = ranges < 1 ? 1 : ranges > most ? most : ranges;
+    s.split_keys = (int)(((p->Lk + ranges - 1) / ranges + 63) / 64 * 64);
     s.k_split = (p->Lk + s.split_keys - 1) / s.split_keys;
   }
+  s.stream = s.split_keys > fit;
   s.unit = s.stream ? 8 : 1;
   const int64_t groups = cus / (slices * s.k_split);
   if (groups >= 1 && (s.QB + groups - 1) / groups <= 8) s.unit = (int)((s.QB + groups - 1) / groups);
@@ -687,7 +695,7 @@ int fgattn_cross_backward(const void* q, const void* k, const void* v, const voi
   a.B = p->B; a.H = p->H; a.Hkv = p->Hkv; a.group = p->H / p->Hkv; a.Lq = p->Lq; a.Lk = p->Lk;
   a.rows = a.group * p->Lq; a.QB = s.QB; a.unit = s.unit; a.QU = s.QU; a.dq_units = p->B * p->Hkv * s.k_split * s.QU;
   a.k_split = s.k_split; a.split_keys = s.split_keys;
-  a.own_delta = p->Lk <= fgx::kOwnDelta;
+  a.own_delta = p->Lk <= fgx::kOwnDelta;   // (one range, resident)
   a.KB = s.KB; a.n_split = s.n_split; a.units = s.units; a.units_per_split = s.units_per_split;
   a.scale = p->scale;
   a.c_log2 = p->scale * 1.44269504088896340736f;

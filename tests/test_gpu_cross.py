@@ -60,6 +60,11 @@ CASES = [
     (2, 9, 2, 999, 661, 64, "blhd", None, None, [661, 64]),
     (1, 24, 1, 3001, 320, 128, "bhld", None, None, [289]),                # all of LDS
     (2, 17, 1, 1301, 640, 64, "bhld", None, [1301, 1300], [640, 577]),
+    (1, 2, 1, 1, 30011, 128, "bhld", None, None, None),                   # the backward call's ranges of keys, in LDS
+    (1, 16, 1, 250, 7000, 128, "blhd", None, [249], [6990]),              # and through rings
+    (2, 5, 2, 61, 9001, 64, "bhld", None, None, [9001, 1000]),
+    (2, 12, 1, 1100, 128, 128, "bhld", None, None, [128, 1]),             # the last length whose D is summed over the keys
+    (2, 3, 1, 400, 129, 64, "blhd", None, None, [129, 2]),
 ]
 IDS = ["-".join(str(x) for x in c[:7]) for c in CASES]
 
