@@ -19,10 +19,10 @@ namespace fgx {
 
 using namespace fg;
 
-// A workgroup per query row.  Every wave has all ranges' weights in its lanes and adds up every fourth range's row; the four sums
+// More than kFewSplits ranges: a workgroup per query row.  Every wave has all ranges' weights in its lanes and adds up every fourth range's row; the four sums
 // meet in LDS.  Bound: latency.  With one wave per row and its loads one after the other 64 ranges of eight rows took 20 us
 // more.
-constexpr int kMaxSplits = 64;
+constexpr int kMaxSplits = 64, kFewSplits = 8;
 struct JoinArgs {
   const float* part_o;
   const float* part_ml;
@@ -30,7 +30,7 @@ struct JoinArgs {
   float* lse;
   const int32_t* q_lens;
   int64_t o_sb, o_sh, o_sl;
-  int32_t Hkv, Lq, rows, group, QB, n_split;   // rows = group * Lq
+  int32_t Hkv, Lq, rows, group, QB, n_split, n_rows;   // rows = group * Lq of a key head; n_rows of all
   float c_log2, scale_abs;
 };
 template <int D>
@@ -88,8 +88,58 @@ __global__ void __launch_bounds__(256) join_kernel(const JoinArgs a) {
   if (tid == 0) a.lse[blockIdx.x] = total > 0.0f ? a.scale_abs * top + __logf(total) : -INFINITY;
 }
 
+// Up to kFewSplits ranges, as calls with thousands of rows have them: four elements of a row per thread, every range's in registers at
+// once (N of them, the last one again where there are fewer).  A workgroup per row took 35 us for two ranges of 24000 rows, bound by
+// the workgroups' latency.
+template <int D, int N>
+__global__ void __launch_bounds__(256) join_few_kernel(const JoinArgs a) {
+  constexpr int PER = D / 4;   // threads of a row
+  const unsigned at = blockIdx.x * (256 / PER) + threadIdx.x / PER;
+  const int e = (threadIdx.x % PER) * 4;
+  if (at >= (unsigned)a.n_rows) return;
+  const unsigned slice = at / (unsigned)a.rows, row = at - slice * (unsigned)a.rows;
+  const unsigned b = slice / (unsigned)a.Hkv, hk = slice - b * (unsigned)a.Hkv;
+  const unsigned of_group = row / (unsigned)a.Lq, l = row - of_group * (unsigned)a.Lq;
+  const int64_t first = ((int64_t)slice * a.QB + (row >> 5)) * a.n_split * 32 + (row & 31);   // range s: + 32 s
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + first;
+  const float* src = a.part_o + first * D + e;
+  f32x2 own[N];
+  f32x4 part[N];
+#pragma unroll
+  for (int s = 0; s < N; s++) {
+    const int from = 32 * min(s, a.n_split - 1);
+    own[s] = ml[from];
+    part[s] = *reinterpret_cast<const f32x4*>(src + from * D);
+  }
+  float top = own[0][0];
+#pragma unroll
+  for (int s = 1; s < N; s++) top = fmaxf(top, own[s][0]);
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  float total = 0.0f;
+#pragma unroll
+  for (int s = 0; s < N; s++) {
+    const float w = own[s][0] == -INFINITY || s >= a.n_split ? 0.0f : __builtin_amdgcn_exp2f((own[s][0] - top) * a.c_log2);
+    total += own[s][1] * w;
+    o += part[s] * w;
+  }
+  if (a.q_lens && (int)l >= a.q_lens[b]) return;   // (rows that no range wrote)
+  o *= total > 0.0f ? 1.0f / total : 0.0f;
+  uint16_t* dst = a.out + b * a.o_sb + (int64_t)(hk * a.group + of_group) * a.o_sh + (int64_t)l * a.o_sl + e;
+  *reinterpret_cast<i32x2*>(dst) = __builtin_bit_cast(i32x2, __builtin_convertvector(o, bf16x4));
+  if (e == 0) a.lse[at] = total > 0.0f ? a.scale_abs * top + __logf(total) : -INFINITY;
+}
+template <int D>
+static void launch_join(const JoinArgs& a, hipStream_t stream) {
+  const int rows = a.n_split <= kFewSplits ? 1024 / D : 1;   // of a workgroup
+  const dim3 grid((unsigned)(((int64_t)a.n_rows + rows - 1) / rows));
+  if (a.n_split <= 2) hipLaunchKernelGGL((join_few_kernel<D, 2>), grid, dim3(256), 0, stream, a);
+  else if (a.n_split <= 4) hipLaunchKernelGGL((join_few_kernel<D, 4>), grid, dim3(256), 0, stream, a);
+  else if (a.n_split <= kFewSplits) hipLaunchKernelGGL((join_few_kernel<D, kFewSplits>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(join_kernel<D>, grid, dim3(256), 0, stream, a);
+}
+
 // LDS of a key head's tiles (K and V, 32 keys each) and how many tiles a workgroup can hold.
-static int64_t resident_bytes(const fgattn_cross_params* p) { return ((int64_t)p->Lk + 63) / 64 * 64 * 4 * p->d; }
+static int64_t resident_bytes(int keys, int d) { return ((int64_t)keys + 63) / 64 * 64 * 4 * d; }
 
 struct Plan {
   bool tiles, stream;   // cross_kernel; its keys pass through rings
@@ -104,25 +154,34 @@ static Plan plan_of(const fgattn_cross_params* p, int cus) {
   const int64_t slices = (int64_t)p->B * p->Hkv;
   s.QB = (rows + 31) / 32;
   const int64_t tiles = slices * s.QB;
-  s.stream = resident_bytes(p) > kLdsBytes;
-  // Which way (microseconds of cross_kernel against ranges; 32 to 8192 keys and 8 to 2520 tiles measured).  Keys in LDS: 77 keys
-  // 24 x 1000 tokens 9.6 against 9.4, 12 x 4096 12.7 against 17.1; 226 keys 8 x 64 tokens 9.0 against 9.8, 24 x 1000 11.6
-  // against 50.  Keys through rings, where few tiles' waves take as long as many: 512 keys 12 x 512 tokens 20.5 against 23, 2048
-  // keys 12 x 1000 tokens 54 against 53, 8192 keys 12 x 1000 tokens 197 against 132 and 24 x 1000 198 against 225; d = 64, 2048 keys
-  // 12 x 1000 tokens 40 against 36, 8192 keys 24 x 1000 141 against 110 and 12 x 4096 143 against 162: as many tiles as the root of the
-  // keys asks for.
-  s.tiles = s.stream ? tiles * tiles * p->d >= 9000 * (int64_t)p->Lk : p->Lk <= 160 ? tiles * p->d >= 128 * 1024 : true;
+  s.stream = resident_bytes(p->Lk, p->d) > kLdsBytes;
+  // Which way (microseconds of cross_kernel against ranges in single waves; 32 to 8192 keys, 8 to 2520 tiles measured).  Keys in LDS:
+  // 77 keys 24 x 1000 tokens 10.0 against 9.2, 12 x 4096 12.8 against 16.9; 226 keys 8 x 64 tokens 9.0 against 8.8, 24 x 1000 11.6
+  // against 26.7.  More keys: 512 keys 8 x 256 tokens 12.4 against 10.6, 12 x 512 15.6 against 18.4; 2048 keys 8 x 64 tokens 12.7
+  // against 11.5, 8 x 256 17.8 against 22.8; 8192 keys 8 x 256 tokens 32 against 26, 12 x 512 49 against 69.  With d = 64 twice
+  // as many single waves are resident: 2048 keys 24 x 1000 tokens 44 against 32, 8192 keys 12 x 4096 tokens 145 against 162.
+  if (!s.stream) s.tiles = p->Lk <= 160 ? tiles * p->d >= 128 * 1024 : true;
+  else if (p->d == 64) s.tiles = tiles >= 1280;
+  else s.tiles = tiles * tiles >= p->Lk && tiles * p->Lk >= 65536;
   s.n_split = 1;
   s.split_keys = p->Lk;
-  s.items = tiles;
-  // Units of cross_kernel: a tile, or with rings, where the waves go through the keys together, one for every wave.  Where a wave has no
-  // more than one tile, as many as leave no workgroup with tiles of two key heads, whose K and V it would have to
-  // wait for twice (226 keys, 12 x 1000 tokens).
-  const int waves = s.stream ? kWavesRings : p->d == 64 ? kWaves64 : kWaves128;
-  s.unit = s.stream ? waves : 1;
-  const int64_t groups = cus / slices;
-  if (groups >= 1 && (s.QB + groups - 1) / groups <= waves) s.unit = (int)((s.QB + groups - 1) / groups);
-  if (!s.tiles) {
+  const int waves_fit = p->d == 64 ? kWaves64 : kWaves128;
+  if (s.tiles) {
+    // as many ranges of keys as give 256 compute units a workgroup with a tile for each of its waves, where that saves more than the
+    // joining takes (1.45 us per 64 keys against 2 us and 1 us per 64 tiles: 512 keys 12 x 512 tokens 15.6 in two ranges, 20.5 in
+    // one, 24 x 1000 tokens 24.5 and 20.4; 2048 keys 24 x 1000 tokens 49 and 57)
+    if (s.stream && p->Lk * 7LL >= 10 * (128 + tiles)) {
+      int64_t n = 256 / (slices * ((s.QB + waves_fit - 1) / waves_fit));
+      const int64_t most = p->Lk / 256;
+      n = n > most ? most : n;
+      n = n > kMaxSplits ? kMaxSplits : n;
+      if (n > 1) {
+        s.split_keys = (int)(((p->Lk + n - 1) / n + 63) / 64 * 64);
+        s.n_split = (p->Lk + s.split_keys - 1) / s.split_keys;
+      }
+    }
+    s.stream = resident_bytes(s.split_keys, p->d) > kLdsBytes;
+  } else {
     const int64_t want = (1024 + tiles - 1) / tiles;
     const int most = (p->Lk + 127) / 128;
     int n = (int)(want < most ? want : most);
@@ -131,12 +190,19 @@ static Plan plan_of(const fgattn_cross_params* p, int cus) {
       s.split_keys = ((p->Lk + n - 1) / n + 31) / 32 * 32;
       s.n_split = (p->Lk + s.split_keys - 1) / s.split_keys;
     }
-    s.items = tiles * s.n_split;
   }
+  s.items = tiles * s.n_split;
+  // Units of cross_kernel: a tile, or with rings, where the waves go through the keys together, one for every wave.  Where a wave has no
+  // more than one tile, as many as leave no workgroup with tiles of two key heads, whose K and V it would have to
+  // wait for twice (226 keys, 12 x 1000 tokens 16.4 -> 10.4 us).
+  const int waves = s.stream ? kWavesRings : waves_fit;
+  s.unit = s.stream ? waves : 1;
+  const int64_t groups = cus / (slices * s.n_split);
+  if (groups >= 1 && (s.QB + groups - 1) / groups <= waves) s.unit = (int)((s.QB + groups - 1) / groups);
   return s;
 }
 
-template <int D, int WV, bool STREAM>
+template <int D, int WV, bool STREAM, bool SPLIT>
 static int launch_cross(const CrossArgs& a, int lds, int cus, hipStream_t stream) {
   static std::mutex mutex;
   static bool ready[64];
@@ -145,14 +211,21 @@ static int launch_cross(const CrossArgs& a, int lds, int cus, hipStream_t stream
   {
     std::lock_guard<std::mutex> lock(mutex);
     if (!ready[dev]) {
-      if (hipFuncSetAttribute(reinterpret_cast<const void*>(cross_kernel<D, WV, STREAM>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes) !=
-          hipSuccess)
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(cross_kernel<D, WV, STREAM, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                              kLdsBytes) != hipSuccess)
         return FGATTN_E_DEVICE;
       ready[dev] = true;
     }
   }
-  hipLaunchKernelGGL((cross_kernel<D, WV, STREAM>), dim3(a.units < cus ? a.units : cus), dim3(WV * 64), lds, stream, a);
+  hipLaunchKernelGGL((cross_kernel<D, WV, STREAM, SPLIT>), dim3(a.units < cus ? a.units : cus), dim3(WV * 64), lds, stream, a);
   return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;
+}
+template <int D>
+static int launch_tiles(const CrossArgs& a, bool rings, int lds, int cus, hipStream_t stream) {
+  constexpr int WV = D == 64 ? kWaves64 : kWaves128;
+  if (rings)
+    return a.n_split > 1 ? launch_cross<D, kWavesRings, true, true>(a, lds, cus, stream) : launch_cross<D, kWavesRings, true, false>(a, lds, cus, stream);
+  return a.n_split > 1 ? launch_cross<D, WV, false, true>(a, lds, cus, stream) : launch_cross<D, WV, false, false>(a, lds, cus, stream);
 }
 
 template <int D>
@@ -230,16 +303,17 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
     c.Hkv = p->Hkv; c.group = a.group; c.Lq = p->Lq; c.Lk = p->Lk; c.rows = a.L; c.QB = s.QB;
     c.unit = s.unit;
     c.QU = (s.QB + c.unit - 1) / c.unit;
-    c.units = p->B * p->Hkv * c.QU;
+    c.n_split = s.n_split;
+    c.split_keys = s.split_keys;
+    c.part_o = a.part_o;
+    c.part_ml = a.part_ml;
+    c.units = p->B * p->Hkv * s.n_split * c.QU;
     c.c_log2 = a.c_log2; c.lazy_raw = a.lazy_raw; c.scale_abs = a.scale_abs; c.q_sign = a.q_sign;
-    if (s.stream)
-      return p->d == 64 ? fgx::launch_cross<64, fgx::kWavesRings, true>(c, fgx::kLdsBytes, cus, stream)
-                        : fgx::launch_cross<128, fgx::kWavesRings, true>(c, fgx::kLdsBytes, cus, stream);
-    const int lds = (int)fgx::resident_bytes(p);
-    return p->d == 64 ? fgx::launch_cross<64, fgx::kWaves64, false>(c, lds, cus, stream)
-                      : fgx::launch_cross<128, fgx::kWaves128, false>(c, lds, cus, stream);
+    const int lds = s.stream ? fgx::kLdsBytes : (int)fgx::resident_bytes(s.split_keys, p->d);
+    rc = p->d == 64 ? fgx::launch_tiles<64>(c, s.stream, lds, cus, stream) : fgx::launch_tiles<128>(c, s.stream, lds, cus, stream);
+  } else {
+    rc = p->d == 64 ? fgx::launch_ranges<64>(a, cus, stream) : fgx::launch_ranges<128>(a, cus, stream);
   }
-  rc = p->d == 64 ? fgx::launch_ranges<64>(a, cus, stream) : fgx::launch_ranges<128>(a, cus, stream);
   if (rc || s.n_split == 1) return rc;
   fgx::JoinArgs j = {};
   j.part_o = a.part_o;
@@ -256,9 +330,9 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
   j.n_split = s.n_split;
   j.c_log2 = a.c_log2;
   j.scale_abs = sabs;
-  const dim3 grid((unsigned)p->B * p->H * p->Lq);
-  if (p->d == 64) hipLaunchKernelGGL(fgx::join_kernel<64>, grid, dim3(256), 0, stream, j);
-  else hipLaunchKernelGGL(fgx::join_kernel<128>, grid, dim3(256), 0, stream, j);
+  j.n_rows = p->B * p->H * p->Lq;
+  if (p->d == 64) fgx::launch_join<64>(j, stream);
+  else fgx::launch_join<128>(j, stream);
   return hipGetLastError() == hipSuccess ? FGATTN_OK : FGATTN_E_DEVICE;
 }
 

@@ -24,7 +24,10 @@ struct CrossArgs {
   const int32_t *q_lens, *k_lens;
   int64_t q_sb, q_sh, q_sl, k_sb, k_sh, k_sl, v_sb, v_sh, v_sl, o_sb, o_sh, o_sl;
   int32_t Hkv, group, Lq, Lk, rows, QB;   // rows = group * Lq of a key head; QB = tiles of 32 of them
-  int32_t unit, QU, units;                // workgroups share out units of `unit` tiles: QU of a key head, units of all
+  int32_t unit, QU, units;                // workgroups share out units of `unit` tiles: QU of a range of a key head's keys, units of all
+  int32_t n_split, split_keys;            // ranges of keys, as in FwdArgs
+  float* part_o;
+  float* part_ml;
   float c_log2, lazy_raw, scale_abs;
   uint32_t q_sign;
 };
@@ -70,7 +73,9 @@ __device__ __forceinline__ void store_row16(uint16_t* row, const f32x16 (&acc)[D
   }
 }
 
-template <int D, int WV, bool STREAM>
+// SPLIT: the keys are split into ranges (a.n_split of them), whose parts a kernel of their own joins.  (A template parameter: with a
+// branch at run time the kernel with rings spilled eleven more registers: 12 heads x 32760 tokens to 512 keys 128-135 us, 120-126 without.)
+template <int D, int WV, bool STREAM, bool SPLIT>
 __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs a) {
   constexpr int CH = D / 8, ROWB = D * 2, RPI = 64 / CH, TB = 32 * ROWB, SSTEPS = D / 16, DBLK = D / 32, NE = SSTEPS;
   // Pairs of key tiles.  Resident: pair p's K and V in slot p.  STREAM: rings of SLOTS slots, K's and V's.
@@ -103,17 +108,20 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
 
   bool again = false;
   while (at_unit < end_unit) {   // one key head
-    const int slice = at_unit / a.QU, first_unit = at_unit - slice * a.QU, first = first_unit * a.unit;
+    const int part = at_unit / a.QU, first_unit = at_unit - part * a.QU, first = first_unit * a.unit;
+    const int slice = SPLIT ? part / a.n_split : part, split = SPLIT ? part - slice * a.n_split : 0;
     const int b = slice / a.Hkv, hk = slice - b * a.Hkv;
     const int n_here = min(a.QU - first_unit, end_unit - at_unit);
     at_unit += n_here;
     const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
-    const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+    const int key0 = SPLIT ? split * a.split_keys : 0;   // (the keys' numbers below begin at 0 with this one)
+    int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
+    if constexpr (SPLIT) k_len = max(0, min(k_len - key0, a.split_keys));
     const int nt = ((k_len + 63) >> 6) * 2;   // (an even number: scores and probabilities of even and odd tiles have registers of their own)
     // (with one query head per key head the rows behind a shorter sequence are whole tiles at the end)
     const int last = min(first + n_here * a.unit, a.group == 1 ? (q_len + 31) >> 5 : a.QB);
-    const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh;
-    const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh;
+    const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh + key0 * a.k_sl;
+    const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh + key0 * a.v_sl;
     if (again) __syncthreads();   // every wave is done with the head before
     again = true;
     // Rows r .. of pair `pair` of K or V -> LDS.  Rows past the last key are read as the last one: finite wherever the tensor is, and
@@ -190,6 +198,19 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       int head, pos;
       const bool valid = place(jj, head, pos);
       const float l_tot = lane_pair_sum(l);
+      if constexpr (SPLIT) {   // (see the end of fgattn_fwd_kernel)
+        if (valid) {
+          const int64_t at = (((int64_t)slice * a.QB + jj) * a.n_split + split) * 32 + ln;
+          float* op = a.part_o + at * D;
+#pragma unroll
+          for (int db = 0; db < DBLK; db++)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; r4++)
+              *reinterpret_cast<f32x4*>(op + 32 * db + 8 * r4 + 4 * g) = f32x4{O[db][4 * r4], O[db][4 * r4 + 1], O[db][4 * r4 + 2], O[db][4 * r4 + 3]};
+          if (g == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * at) = f32x2{m, l_tot};
+        }
+        return;
+      }
       const float inv = l_tot > 0.0f ? 1.0f / l_tot : 0.0f;
       store_row16<D>(obase + head * a.o_sh + (int64_t)pos * a.o_sl, O, inv, g, valid);
       if (valid && g == 0) a.lse[(int64_t)slice * a.rows + jj * 32 + ln] = l_tot > 0.0f ? a.scale_abs * m + __logf(l_tot) : -INFINITY;
