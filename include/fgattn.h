@@ -240,7 +240,7 @@ typedef struct fgattn_rope_axis {
  *   axes : HOST array of n_axes (1 .. 3) axes; rows = the product of the sizes, <= 2^24; the pairs sum to at most 128.
  * Errors: FGATTN_E_SHAPE for sizes out of range, FGATTN_E_SCALE for numbers that are not finite or not as above.
  */
-int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, float mscale, float* cos, float* sin, void* stream);
+int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, double mscale, float* cos, float* sin, void* stream);
 
 enum { FGATTN_ROPE_INTERLEAVED = 0,   /* pair j of a head = its elements 2j and 2j + 1 */
        FGATTN_ROPE_HALF = 1 };        /* pair j = elements j and j + rot_dims / 2 */

@@ -342,18 +342,32 @@ __global__ void __launch_bounds__(kThreads) rope_grad_kernel(const RopeArgs a) {
         }
       }
     }
-    if (a.partial != nullptr) {   // (the same in all threads)
-      if (t) __syncthreads();
-#pragma unroll
-      for (int i = 0; i < V; i++) sums[tid / LPR][(tid % LPR) * V + i] = dw[i];
-      __syncthreads();
-      float* out = a.partial + (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 + t) * a.d;
-      for (int e = tid; e < a.d; e += kThreads) {
-        float sum = 0.0f;
-        for (int k = 0; k < ROWS; k++) sum += sums[k][e];
-        out[e] = sum;
-      }
+    if (a.partial == nullptr) continue;   // (the same in all threads, like the next condition)
+    float* out = a.partial + (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 + t) * a.d;
+    if (h0 >= h1) {
+      if (tid < a.d) out[tid] = 0.0f;
+      continue;
     }
+    if (t) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; i++) sums[tid / LPR][(tid % LPR) * V + i] = dw[i];
+    __syncthreads();
+    // LPR * V columns of ROWS values: a column's share per thread, then the shares
+    constexpr int COLS = LPR * V, SHARES = kThreads / COLS, PER = ROWS / SHARES;
+    static_assert(COLS <= kThreads && PER >= 1 && SHARES * PER == ROWS, "columns and shares");
+    const int col = tid % COLS, share = tid / COLS;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < PER; k++) sum += sums[share * PER + k][col];
+    if constexpr (SHARES > 1) {
+      __syncthreads();
+      sums[share][col] = sum;
+      __syncthreads();
+      sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < SHARES; k++) sum += sums[k][col];
+    }
+    if (share == 0 && col < a.d) out[col] = sum;
   }
 }
 
@@ -525,7 +539,7 @@ static int run_rows(const void* q, const void* k, const void* qw, const void* kw
 
 extern "C" {
 
-int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, float mscale, float* cos, float* sin, void* stream) {
+int fgattn_rope_table(const fgattn_rope_axis* axes, int n_axes, double mscale, float* cos, float* sin, void* stream) {
   if (!axes || !cos || !sin) return FGATTN_E_NULL;
   if (n_axes < 1 || n_axes > 3) return FGATTN_E_SHAPE;
   if (!isfinite(mscale)) return FGATTN_E_SCALE;

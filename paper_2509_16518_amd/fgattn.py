@@ -96,7 +96,7 @@ def lib():
         L.fgattn_group_emit.argtypes = [pp, ctypes.c_int, vp, vp, vp, vp, ctypes.c_int64, vp, ctypes.c_size_t, vp]
         L.fgattn_group_emit.restype = ctypes.c_int
         rp, xp, sz = ctypes.POINTER(FgattnRopeParams), ctypes.POINTER(FgattnCrossParams), ctypes.c_size_t
-        L.fgattn_rope_table.argtypes = [ctypes.POINTER(FgattnRopeAxis), ctypes.c_int, ctypes.c_float, vp, vp, vp]
+        L.fgattn_rope_table.argtypes = [ctypes.POINTER(FgattnRopeAxis), ctypes.c_int, ctypes.c_double, vp, vp, vp]
         L.fgattn_rope_table.restype = ctypes.c_int
         L.fgattn_rope_forward.argtypes = [vp] * 6 + [ctypes.c_int32, vp, rp, vp, vp, vp]
         L.fgattn_rope_forward.restype = ctypes.c_int

@@ -232,3 +232,50 @@ def test_wide_strides():
         result.append([out, lse] + grads)
     for a, b in zip(*result):
         assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    # two problems on two streams, workspaces of their own: each as by itself
+    x = Problem(CASES[11], seed=31), Problem(CASES[18], seed=32)
+    for t in x:
+        t.forward()
+        t.want = [t.out.clone(), t.lse.clone()] + t.backward()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [None, None]
+    for _ in range(3):
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        for n, (t, s) in enumerate(zip(x, streams)):
+            with torch.cuda.stream(s):
+                t.out.fill_(99.0)
+                t.forward()
+                got[n] = t.backward()
+        torch.cuda.synchronize()
+        for n, t in enumerate(x):
+            for a, b in zip([t.out, t.lse] + got[n], t.want):
+                assert torch.equal(a, b)
+
+
+def test_the_most_keys():
+    # nearly 2^24 keys (byte offsets up to 2 GiB), scores 0: the result is the mean of the values, dv the same row everywhere, dk zero
+    L, d, rows = 2 ** 24 - 5, 64, 3
+    k, v = (torch.empty((1, 1, L, d), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(n)) for n in (1, 2))
+    q = torch.zeros((1, 1, rows, d), dtype=torch.bfloat16, device="cuda")
+    dout = torch.randn((1, 1, rows, d), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty((1, 1, rows), device="cuda")
+    p = F.make_cross_params(q, k, v, out, 0.125)
+    F.fgattn_cross_forward(q, k, v, p, out, lse, torch.empty(F.fgattn_cross_workspace_bytes(p), dtype=torch.uint8, device="cuda"))
+    mean = v.sum(2, dtype=torch.float64) / L
+    # 64 ranges of 2^18 keys, 16 keys per matrix instruction: 2^14 additions of fp32 to sums of 2^18 values of size 1 (below 6 * 2^9)
+    assert ((out.double() - mean[:, :, None]).abs() <= 2.0 ** -8 * mean.abs()[:, :, None] + 2 ** 14 * 2.0 ** -24 * 6 * 2 ** 9 * 64 / L).all()
+    # a logarithm to base 2 near 24, good to one step there (2^-19), times ln 2: 0.7 * 2^-19; that product and its sum with the maximum
+    # each rounded near 16.6 (half a step, 2^-20): 1.7 * 2^-19 in all
+    assert ((lse.double() - math.log(L)).abs() <= 2.0 ** -18).all()
+    grads = [torch.empty_like(t) for t in (q, k, v)]
+    p = F.make_cross_params(q, k, v, out, 0.125, dout, *grads)
+    F.fgattn_cross_backward(q, k, v, out, lse, dout, p, *grads, torch.empty(F.fgattn_cross_backward_workspace_bytes(p), dtype=torch.uint8, device="cuda"))
+    assert (grads[1] == 0).all() and torch.isfinite(grads[0]).all()
+    dv = dout.double().sum(2) / L
+    bound = 2 * 2.0 ** -8 * dout.double().abs().sum(2) / L       # P rounded to bf16, the sum rounded
+    for n in range(0, L, 2 ** 21):
+        assert ((grads[2][:, :, n:n + 2 ** 21].double() - dv[:, :, None]).abs() <= bound[:, :, None]).all()

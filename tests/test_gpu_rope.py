@@ -37,7 +37,7 @@ def test_table(name, mscale):
     rows, pairs = math.prod(a[0] for a in axes), sum(a[1] for a in axes)
     cos, sin = (torch.full((rows + 1, pairs), 7.0, device="cuda") for _ in "cs")
     F.fgattn_rope_table(axes, cos[:rows], sin[:rows], mscale=mscale)
-    c, s, angle = P.table(axes, float(torch.tensor(mscale, dtype=FP32)))
+    c, s, angle = P.table(axes, mscale)
     # one rounding to fp32; angles and 16 turns in 64 bits (each to a few steps of the angle, both sides)
     slack = mscale * (angle.abs() * 2.0 ** -48 + 2.0 ** -44)
     within(cos[:rows].cpu(), c, P.F32 * c.abs() + slack, name)
