@@ -32,7 +32,7 @@ enum {
   FGATTN_OK = 0,
   FGATTN_E_NULL = -1,        /* a required pointer is NULL */
   FGATTN_E_SHAPE = -2,       /* B,H,L < 1; L > 2^24; d not in {64,128}; M not in {16,32,64,128}; N < 1;
-                                L+N overflows int32 */
+                                L+N overflows int32 (the rotary and cross attention calls: see there) */
   FGATTN_E_STRIDE = -3,      /* a stride is not a multiple of 8 elements, a row stride is smaller than d, or a K/V
                                 (batch, head) slice spans 4 GiB or more, or a row stride is 16 MiB or more */
   FGATTN_E_ALIGN = -4,       /* q/k/v/out not 16-byte aligned, or workspace not 256-byte aligned */
@@ -325,10 +325,13 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
                          void* stream);
 
 /*
+ * (Results of these two calls must not overlap what they read.)
+ *
  * Its gradients: dq, dk, dv (bf16, every element written: zeros for rows from q_lens[b] and keys from k_lens[b] on) from
  * the forward call's inputs and results and dout, the gradient of out (rows from q_lens[b] on are not read, of out and
  * lse neither).  Where query heads share a key head its gradient is the sum of theirs.  P and dS are rounded to
- * bf16 for the matrix instructions, all sums are fp32, the results are rounded once.
+ * bf16 for the matrix instructions, all sums are fp32, the results are rounded once.  A (batch, head) slice of q and of dout
+ * ends below 4 GiB, as one of k and v does in both calls (FGATTN_E_STRIDE).
  */
 size_t fgattn_cross_backward_workspace_bytes(const fgattn_cross_params* p);
 int fgattn_cross_backward(const void* q, const void* k, const void* v, const void* out, const float* lse, const void* dout,

@@ -451,11 +451,11 @@ const char* fgattn_strerror(int code) {
   switch (code) {
     case FGATTN_OK: return "ok";
     case FGATTN_E_NULL: return "a required pointer is NULL";
-    case FGATTN_E_SHAPE: return "unsupported shape (need B,H,L >= 1, d in {64,128}, M in {16,32,64,128}, N >= 1)";
-    case FGATTN_E_STRIDE: return "strides must be multiples of 8 elements and row strides >= d";
-    case FGATTN_E_ALIGN: return "q/k/v/out must be 16-byte aligned and the workspace 256-byte aligned";
-    case FGATTN_E_WORKSPACE: return "workspace too small (see fgattn_workspace_bytes)";
-    case FGATTN_E_SCALE: return "scale must be finite";
+    case FGATTN_E_SHAPE: return "unsupported shape (attention: B,H,L >= 1, d in {64,128}, M in {16,32,64,128}, N >= 1; rotary calls: d a multiple of 8 up to 256)";
+    case FGATTN_E_STRIDE: return "strides must be multiples of 8 elements and row strides >= d (of results every stride), slices below 4 GiB";
+    case FGATTN_E_ALIGN: return "tensors must be 16-byte aligned (fp32 and int32 arrays 4-byte) and the workspace 256-byte aligned";
+    case FGATTN_E_WORKSPACE: return "workspace too small (see fgattn_workspace_bytes and its like for other calls)";
+    case FGATTN_E_SCALE: return "scale, eps and the numbers of a rotary axis must be finite and in range";
     case FGATTN_E_DEVICE: return "no gfx950 device current, or a HIP runtime call failed";
     case FGATTN_E_MASK: return "mask failed validation";
     case FGATTN_E_FLAGS: return "unknown flag bits";
