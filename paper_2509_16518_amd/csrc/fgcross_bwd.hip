@@ -121,17 +121,22 @@ __device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D /
     }
 }
 
+// Waves of a workgroup: eight, or with rings two workgroups of four on a compute unit, of which one computes while the other one waits
+// for its rows.
+constexpr int dq_waves(bool stream) { return stream ? 4 : 8; }
+constexpr int kDqRingBytes = kLdsBytes / 2;
+
 // A wave's work on a query tile is a software pipeline over its key tiles: step n runs S(n+1) = K(n+1) Q^T and dP(n+1) = V(n+1) dO^T side by
 // side with the exponentials and products that make dS(n) of S(n) and dP(n), then dQ += K(n)^T dS(n)^T.  Bound: the matrix
 // pipe (24 instructions per tile) beside about 90 vector instructions.  The next query tile's rows are not loaded ahead: there
 // are no registers left for them, and the other wave of the SIMD computes meanwhile.
 template <int D, bool STREAM>
-__global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
+__global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdArgs a) {
   using T = Tile<D>;
-  constexpr int WV = 8, TB = T::BYTES, RPI = T::RPI, NE = T::SSTEPS, DBLK = T::DBLK;
-  // pairs of key tiles: slot s holds 64 rows of K, then 64 of V
-  constexpr int PB2 = 2 * TB, SLOTS = kLdsBytes / (2 * PB2), IPW = 64 / RPI / WV;
-  static_assert(IPW * RPI * WV == 64 && SLOTS >= 4, "every wave fetches the same number of rows");
+  constexpr int WV = dq_waves(STREAM), TB = T::BYTES, RPI = T::RPI, NE = T::SSTEPS, DBLK = T::DBLK;
+  // slot s holds 32 rows of K, then 32 of V
+  constexpr int SLOT = 2 * TB, SLOTS = kDqRingBytes / SLOT, IPW = 32 / RPI / WV;
+  static_assert(!STREAM || (IPW * RPI * WV == 32 && SLOTS >= 5), "every wave fetches the same number of rows");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -165,19 +170,19 @@ __global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
     const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh + key0 * a.v_sl;
     if (again) __syncthreads();   // every wave is done with the keys before
     again = true;
-    // Rows r .. of pair `pair` of K or V -> LDS.  Rows past the last key are read as the last one: finite wherever the tensor is, and
+    // Rows r .. of key tile t of K or V -> LDS.  Rows past the last key are read as the last one: finite wherever the tensor is, and
     // multiplied by zero.
-    auto fetch = [&](const uint16_t* base, unsigned row_bytes, int pair, int r, unsigned at) {
-      const int key = min(pair * 64 + r + lrow, cnt - 1);
-      gather16(base, __umul24((unsigned)key, row_bytes) + (unsigned)((pc ^ T::swz((r + lrow) & 31)) << 4), at + r * T::ROWB);
+    auto fetch = [&](const uint16_t* base, unsigned row_bytes, int t, int r, unsigned at) {
+      const int key = min(t * 32 + r + lrow, cnt - 1);
+      gather16(base, __umul24((unsigned)key, row_bytes) + (unsigned)((pc ^ T::swz(r + lrow)) << 4), at + r * T::ROWB);
     };
-    int next = 0, next_slot = 0;   // STREAM: the pair that is fetched next and the slot it goes to
+    int next = 0, next_slot = 0;   // STREAM: the tile that is fetched next and the slot it goes to
     auto fetch_kv = [&](int i) {   // load i of 2 IPW of this wave
       const int r = (wv * IPW + (i < IPW ? i : i - IPW)) * RPI;
-      if (i < IPW) fetch(kbase, k_rowb, next, r, lds0 + next_slot * 2 * PB2);
-      else fetch(vbase, v_rowb, next, r, lds0 + next_slot * 2 * PB2 + PB2);
+      if (i < IPW) fetch(kbase, k_rowb, next, r, lds0 + next_slot * SLOT);
+      else fetch(vbase, v_rowb, next, r, lds0 + next_slot * SLOT + TB);
       if (i + 1 < 2 * IPW) return;
-      next = next + 1 == np ? 0 : next + 1;
+      next = next + 1 == 2 * np ? 0 : next + 1;
       next_slot = next_slot + 1 == SLOTS ? 0 : next_slot + 1;
     };
     if constexpr (STREAM) {
@@ -185,16 +190,16 @@ __global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
         for (int n = 0; n + 1 < SLOTS; n++)
           for (int i = 0; i < 2 * IPW; i++) fetch_kv(i);
     } else {
-      for (int i = wv; i < np * (64 / RPI); i += WV) {
-        const int pair = i / (64 / RPI), r = (i - pair * (64 / RPI)) * RPI;
-        fetch(kbase, k_rowb, pair, r, lds0 + pair * 2 * PB2);
-        fetch(vbase, v_rowb, pair, r, lds0 + pair * 2 * PB2 + PB2);
+      for (int i = wv; i < 2 * np * (32 / RPI); i += WV) {
+        const int t = i / (32 / RPI), r = (i - t * (32 / RPI)) * RPI;
+        fetch(kbase, k_rowb, t, r, lds0 + t * SLOT);
+        fetch(vbase, v_rowb, t, r, lds0 + t * SLOT + TB);
       }
     }
     wait_vmem_all();
     __syncthreads();
 
-    int slot = 0;   // STREAM: of the pair whose dS comes next
+    int slot = 0;   // STREAM: of the tile whose dS comes next
     const int turns = (last - first + WV - 1) / WV;
     for (int turn = 0; turn < turns; turn++) {
       const int j = first + turn * WV + wv;
@@ -242,14 +247,14 @@ __global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
       delta = lane_pair_sum(delta);
       const float lse2 = counts ? a.lse[at] * 1.44269504088896340736f : INFINITY;
       constexpr int AHEAD = 2;
-      // Sn, dPn of the tile at k_at (its V 64 rows further on)
+      // Sn, dPn of the tile at k_at (its V 32 rows further on)
       auto scores = [&](int k_at, f32x16& Sn, f32x16& dPn, auto between) {
         int kb = rd.row_off + k_at;
         asm volatile("" : "+v"(kb));   // (one addition here, and plain XORs with constants below)
         bf16x8 kf[NE], vf[NE];
         auto read = [&](int s) {
           kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + (kb ^ (32 * s))));
-          vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + PB2 + (kb ^ (32 * s))));
+          vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + TB + (kb ^ (32 * s))));
         };
 #pragma unroll
         for (int s = 0; s < AHEAD; s++) read(s);
@@ -309,8 +314,8 @@ __global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
           }
         };
         for (int p = 0; p < np; p++) {
-          scores(p * 2 * PB2, SA, DA, [](auto) {});
-          scores(p * 2 * PB2 + TB, SB, DB, [&](auto ec) {
+          scores(2 * p * SLOT, SA, DA, [](auto) {});
+          scores((2 * p + 1) * SLOT, SB, DB, [&](auto ec) {
             if constexpr (decltype(ec)::value == 0) sum(2 * p, SA, DA);
           });
           sum(2 * p + 1, SB, DB);
@@ -326,33 +331,44 @@ __global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; r++) acc[db][r] = 0.0f;
       if (np > 0) {
-        int k_at = STREAM ? slot * 2 * PB2 : 0;
-        scores(k_at, SA, DA, [](auto) {});
-        for (int p = 0; p < np; p++) {
-          int k_next = k_at + 2 * PB2;
+        int k_at = STREAM ? slot * SLOT : 0;
+        // Where the tile after the one at k_at lies.  STREAM: it has arrived (what was fetched in the SLOTS - 3 steps before may still be
+        // under way), and every wave is done with the tile before this one, into whose slot the one SLOTS - 1 ahead follows.
+        auto advance = [&]() {
           if constexpr (STREAM) {
-            // pair p + 1 has arrived, and every wave is done with pair p - 1: the pair SLOTS - 1 ahead follows into its slot
             wait_vmem_le<(SLOTS - 3) * 2 * IPW>();
             __syncthreads();
             slot = slot + 1 == SLOTS ? 0 : slot + 1;
-            k_next = slot * 2 * PB2;
+            return slot * SLOT;
+          } else {
+            return k_at + SLOT;
           }
+        };
+        auto load = [&](auto ec) {   // between the matrix instructions
+          constexpr int e = decltype(ec)::value, EVERY = NE / (2 * IPW > 0 ? 2 * IPW : 1);
+          if constexpr (STREAM && e % EVERY == 1 % EVERY && e / EVERY < 2 * IPW) fetch_kv(e / EVERY);
+        };
+        scores(k_at, SA, DA, [](auto) {});
+        for (int p = 0; p < np; p++) {
           // tile 2 p + 1 beside tile 2 p
-          scores(k_at + TB, SB, DB, [&](auto ec) {
+          int k_next = advance();
+          scores(k_next, SB, DB, [&](auto ec) {
             form(ec, SA, DA);
-            if constexpr (STREAM && decltype(ec)::value % (NE / 2) == 1 && decltype(ec)::value / (NE / 2) < IPW) fetch_kv(decltype(ec)::value / (NE / 2));
+            load(ec);
           });
           mask(2 * p);
           add(k_at);
+          k_at = k_next;
           // the next pair's first tile beside tile 2 p + 1
+          k_next = advance();
           auto second = [&](auto ec) {
             form(ec, SB, DB);
-            if constexpr (STREAM && decltype(ec)::value % (NE / 2) == 1 && decltype(ec)::value / (NE / 2) < IPW) fetch_kv(IPW + decltype(ec)::value / (NE / 2));
+            load(ec);
           };
           if (p + 1 < np) scores(k_next, SA, DA, second);
           else [&]<int... E>(std::integer_sequence<int, E...>) { (second(std::integral_constant<int, E>()), ...); }(std::make_integer_sequence<int, NE>());
           mask(2 * p + 1);
-          add(k_at + TB);
+          add(k_at);
           k_at = k_next;
         }
       }
@@ -370,7 +386,7 @@ __global__ void __launch_bounds__(512, 2) dq_kernel(const BwdArgs a) {
         store_row16<D>(a.dq + b * a.dq_sb + head * a.dq_sh + (int64_t)pos * a.dq_sl, acc, counts ? a.scale : 0.0f, g, mine);
       }
     }
-    if constexpr (STREAM) wait_vmem_all();   // (pairs that nobody reads; none may land after this workgroup)
+    if constexpr (STREAM) wait_vmem_all();   // (tiles that nobody reads; none may land after this workgroup)
   }
 }
 
@@ -588,9 +604,9 @@ static BwdPlan bwd_plan(const fgattn_cross_params* p, int cus) {
     s.k_split = (p->Lk + s.split_keys - 1) / s.split_keys;
   }
   s.stream = s.split_keys > fit;
-  s.unit = s.stream ? 8 : 1;
-  const int64_t groups = cus / (slices * s.k_split);
-  if (groups >= 1 && (s.QB + groups - 1) / groups <= 8) s.unit = (int)((s.QB + groups - 1) / groups);
+  s.unit = s.stream ? dq_waves(true) : 1;
+  const int64_t groups = (s.stream ? 2 * cus : cus) / (slices * s.k_split);
+  if (groups >= 1 && (s.QB + groups - 1) / groups <= dq_waves(s.stream)) s.unit = (int)((s.QB + groups - 1) / groups);
   s.QU = (s.QB + s.unit - 1) / s.unit;
   auto round = [](size_t x) { return (x + 255) & ~(size_t)255; };
   s.stats_bytes = round((size_t)p->B * p->H * p->Lq * 2 * sizeof(float));
@@ -621,8 +637,9 @@ template <int D>
 static int launch_bwd(BwdArgs& a, const BwdPlan& s, int cus, hipStream_t stream) {
   static bool ready[3][64];
   const int slices = a.B * a.Hkv;
-  const dim3 dq_grid(a.dq_units < cus ? a.dq_units : cus);
-  int rc = s.stream ? launch_lds(dq_kernel<D, true>, kLdsBytes, kLdsBytes, dq_grid, 512, stream, a, ready[0])
+  const int dq_groups = s.stream ? 2 * cus : cus;
+  const dim3 dq_grid(a.dq_units < dq_groups ? a.dq_units : dq_groups);
+  int rc = s.stream ? launch_lds(dq_kernel<D, true>, kDqRingBytes, kDqRingBytes, dq_grid, dq_waves(true) * 64, stream, a, ready[0])
                     : launch_lds(dq_kernel<D, false>, kLdsBytes, (s.split_keys + 63) / 64 * 64 * 4 * D, dq_grid, 512, stream, a, ready[1]);
   if (rc) return rc;
   if (s.k_split > 1) {
