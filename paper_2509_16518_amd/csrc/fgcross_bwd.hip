@@ -122,7 +122,7 @@ __device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D /
 }
 
 // Waves of a workgroup: eight, or with rings two workgroups of four on a compute unit, of which one computes while the other one waits
-// for its rows.
+// for its rows (the whole call for 12 heads x 32760 tokens and 512 keys of 128 elements 404 us, 412 with one of eight; 1024 keys 698, 710).
 constexpr int dq_waves(bool stream) { return stream ? 4 : 8; }
 constexpr int kDqRingBytes = kLdsBytes / 2;
 
@@ -134,9 +134,11 @@ template <int D, bool STREAM>
 __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdArgs a) {
   using T = Tile<D>;
   constexpr int WV = dq_waves(STREAM), TB = T::BYTES, RPI = T::RPI, NE = T::SSTEPS, DBLK = T::DBLK;
-  // slot s holds 32 rows of K, then 32 of V
-  constexpr int SLOT = 2 * TB, SLOTS = kDqRingBytes / SLOT, IPW = 32 / RPI / WV;
-  static_assert(!STREAM || (IPW * RPI * WV == 32 && SLOTS >= 5), "every wave fetches the same number of rows");
+  // Slot s holds TILES key tiles' rows of K, then of V.  With 64 elements a tile is 12 matrix instructions, and a barrier per two of
+  // them costs less than one each (24 heads x 32760 tokens to 1024 keys, the whole call 850 us, 871 with one each).
+  constexpr int TILES = STREAM && D == 64 ? 2 : 1, VO = TILES * TB;
+  constexpr int SLOT = 2 * VO, SLOTS = kDqRingBytes / SLOT, IPW = TILES * 32 / RPI / WV;
+  static_assert(!STREAM || (IPW * RPI * WV == TILES * 32 && SLOTS >= 5), "every wave fetches the same number of rows");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -173,16 +175,16 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
     // Rows r .. of key tile t of K or V -> LDS.  Rows past the last key are read as the last one: finite wherever the tensor is, and
     // multiplied by zero.
     auto fetch = [&](const uint16_t* base, unsigned row_bytes, int t, int r, unsigned at) {
-      const int key = min(t * 32 + r + lrow, cnt - 1);
-      gather16(base, __umul24((unsigned)key, row_bytes) + (unsigned)((pc ^ T::swz(r + lrow)) << 4), at + r * T::ROWB);
+      const int key = min(t * (TILES * 32) + r + lrow, cnt - 1);
+      gather16(base, __umul24((unsigned)key, row_bytes) + (unsigned)((pc ^ T::swz((r + lrow) & 31)) << 4), at + r * T::ROWB);
     };
-    int next = 0, next_slot = 0;   // STREAM: the tile that is fetched next and the slot it goes to
+    int next = 0, next_slot = 0;   // STREAM: what is fetched next (TILES tiles) and the slot it goes to
     auto fetch_kv = [&](int i) {   // load i of 2 IPW of this wave
       const int r = (wv * IPW + (i < IPW ? i : i - IPW)) * RPI;
       if (i < IPW) fetch(kbase, k_rowb, next, r, lds0 + next_slot * SLOT);
-      else fetch(vbase, v_rowb, next, r, lds0 + next_slot * SLOT + TB);
+      else fetch(vbase, v_rowb, next, r, lds0 + next_slot * SLOT + VO);
       if (i + 1 < 2 * IPW) return;
-      next = next + 1 == 2 * np ? 0 : next + 1;
+      next = next + 1 == 2 / TILES * np ? 0 : next + 1;
       next_slot = next_slot + 1 == SLOTS ? 0 : next_slot + 1;
     };
     if constexpr (STREAM) {
@@ -199,7 +201,7 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
     wait_vmem_all();
     __syncthreads();
 
-    int slot = 0;   // STREAM: of the tile whose dS comes next
+    int slot = 0;   // STREAM: of the tile whose dS comes next, and with it the TILES - 1 beside it
     const int turns = (last - first + WV - 1) / WV;
     for (int turn = 0; turn < turns; turn++) {
       const int j = first + turn * WV + wv;
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
         bf16x8 kf[NE], vf[NE];
         auto read = [&](int s) {
           kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + (kb ^ (32 * s))));
-          vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + TB + (kb ^ (32 * s))));
+          vf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(smem + VO + (kb ^ (32 * s))));
         };
 #pragma unroll
         for (int s = 0; s < AHEAD; s++) read(s);
@@ -334,8 +336,9 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
         int k_at = STREAM ? slot * SLOT : 0;
         // Where the tile after the one at k_at lies.  STREAM: it has arrived (what was fetched in the SLOTS - 3 steps before may still be
         // under way), and every wave is done with the tile before this one, into whose slot the one SLOTS - 1 ahead follows.
-        auto advance = [&]() {
+        auto advance = [&](bool odd) {
           if constexpr (STREAM) {
+            if (TILES == 2 && odd) return k_at + TB;
             wait_vmem_le<(SLOTS - 3) * 2 * IPW>();
             __syncthreads();
             slot = slot + 1 == SLOTS ? 0 : slot + 1;
@@ -351,16 +354,16 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
         scores(k_at, SA, DA, [](auto) {});
         for (int p = 0; p < np; p++) {
           // tile 2 p + 1 beside tile 2 p
-          int k_next = advance();
+          int k_next = advance(true);
           scores(k_next, SB, DB, [&](auto ec) {
             form(ec, SA, DA);
-            load(ec);
+            if constexpr (TILES == 1) load(ec);
           });
           mask(2 * p);
           add(k_at);
           k_at = k_next;
           // the next pair's first tile beside tile 2 p + 1
-          k_next = advance();
+          k_next = advance(false);
           auto second = [&](auto ec) {
             form(ec, SB, DB);
             load(ec);
@@ -452,6 +455,9 @@ __global__ void __launch_bounds__(256, 2) dkdv_kernel(const BwdArgs a) {
         hl++;
       }
     };
+    // A wave without keys (never the first, which fetches lse and D) only fetches rows for the others: 77 keys, 12 x 32760 tokens, the
+    // whole call 163 -> 157 us.
+    const bool idle = key0 + wv * 32 >= k_len;
     // (a unit behind the last token of a shorter sequence is fetched as copies of its last row, with P = 0)
     if (u0 < u1) {
       fetch(0);
@@ -462,6 +468,7 @@ __global__ void __launch_bounds__(256, 2) dkdv_kernel(const BwdArgs a) {
       wait_vmem_all();
       __syncthreads();
       if (u + 1 < u1) fetch(slot ^ 1);
+      if (idle) continue;
       const unsigned char* qt = smem + slot * 2 * T::BYTES;
       const unsigned char* dot = qt + T::BYTES;
       const float* stt = stats + slot * 64;

@@ -161,13 +161,9 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
         fetch(vbase, v_rowb, false, pair, r, lds0 + pair * K_STEP + V_OFF);
       }
     }
-    wait_vmem_all();
-    __syncthreads();
-
     int j = first + wv;
     // STREAM: the waves go through the keys together, a wave without a tile of its own along with the others
     const int turns = (last - first + WV - 1) / WV;
-    if (STREAM ? turns <= 0 : j >= last) continue;
     const uint16_t* const qbase = a.q + b * a.q_sb + (int64_t)hk * a.group * a.q_sh;
     uint16_t* const obase = a.out + b * a.o_sb + (int64_t)hk * a.group * a.o_sh;
     // this lane's row of query tile jj: whether it counts, its head inside the group and its token
@@ -185,6 +181,12 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
 #pragma unroll
       for (int s = 0; s < SSTEPS; s++) qn[s] = *reinterpret_cast<const i32x4*>(qp + 32 * s);
     };
+    // Resident keys: the first tile's rows are under way together with them (24 heads x 118800 tokens to 256 keys 464 -> 454 us; with
+    // rings 12 x 32760 tokens to 1024 keys took 206 us for 204).  A wave without a tile reads the last row for nothing.
+    if constexpr (!STREAM) load_q(j);
+    wait_vmem_all();
+    __syncthreads();
+    if (STREAM ? turns <= 0 : j >= last) continue;
     auto take_q = [&]() {
 #pragma unroll
       for (int s = 0; s < SSTEPS; s++) qf[s] = __builtin_bit_cast(bf16x8, qn[s] ^ (int)a.q_sign);
@@ -244,7 +246,7 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FG_LDS s16x4*)(p0 + 8 * ROWB));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    load_q(j);
+    if constexpr (STREAM) load_q(j);
     take_q();
 #pragma unroll
     for (int r = 0; r < 16; r++) SA[r] = 0.0f;
