@@ -248,7 +248,8 @@ enum { FGATTN_FLAG_ROPE_NORM = 1,           /* RMS norm of every row (one head o
        FGATTN_FLAG_ROPE_WEIGHT_FP32 = 2 };  /* the norm weights are fp32 whatever `dtype` is (otherwise of that type) */
 
 typedef struct fgattn_rope_params {
-  int32_t B, Hq, Hk, L, d;       /* batch, heads of q and of k (0: no k), tokens (<= 2^24), head dim: a multiple of 8, 8 .. 256 */
+  int32_t B, Hq, Hk, L, d;       /* batch, heads of q and of k (0: no k; <= 65535 together), tokens (<= 2^24, B * L <= 2^25), head
+                                    dim: a multiple of 8, 8 .. 256 */
   int32_t rot_dims;              /* elements of a head that are turned, from its first on: even, 0 .. d */
   int32_t layout;                /* FGATTN_ROPE_* */
   int32_t dtype;                 /* type of q, k and of the results */

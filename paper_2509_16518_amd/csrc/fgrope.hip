@@ -400,7 +400,8 @@ static int check_params(const fgattn_rope_params* p) {
   if (p->d < 8 || p->d > 256 || p->d % 8 != 0) return FGATTN_E_SHAPE;
   if (p->rot_dims < 0 || p->rot_dims > p->d || p->rot_dims % 2 != 0) return FGATTN_E_SHAPE;
   if (p->layout != FGATTN_ROPE_INTERLEAVED && p->layout != FGATTN_ROPE_HALF) return FGATTN_E_SHAPE;
-  if ((int64_t)p->Hq + p->Hk > 65535 || (int64_t)p->B * p->L > 0x7fff0000LL) return FGATTN_E_SHAPE;
+  // (a workgroup's 256 threads take four tokens or more, and a launch stays below 2^32 threads)
+  if ((int64_t)p->Hq + p->Hk > 65535 || (int64_t)p->B * p->L > (1 << 25)) return FGATTN_E_SHAPE;
   if (p->dtype != FGATTN_BF16 && p->dtype != FGATTN_FP16 && p->dtype != FGATTN_FP32) return FGATTN_E_DTYPE;
   if (p->flags & ~(FGATTN_FLAG_ROPE_NORM | FGATTN_FLAG_ROPE_WEIGHT_FP32)) return FGATTN_E_FLAGS;
   if (!isfinite(p->eps) || p->eps < 0.0f) return FGATTN_E_SCALE;

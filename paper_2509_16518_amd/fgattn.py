@@ -331,6 +331,8 @@ def fgattn_rope_table(axes, cos, sin, mscale=1.0, stream=None):
         _refuse(E_SHAPE)
     rows, pairs, table = 1, 0, []
     for x in axes:
+        if not 3 <= len(x) <= 9:
+            _refuse(E_SHAPE)
         rows, pairs = rows * x[0], pairs + x[1]
         table.append(FgattnRopeAxis(*x, *(0.0, 1.0, 1.0, 0.0, 32.0, 1.0)[len(x) - 3:]))
     device, f32, shape = cos.get_device(), torch.float32, (rows, pairs)
@@ -385,6 +387,8 @@ def _rope_operands(params, q, k, cos, sin, positions, q_weight, k_weight, result
     f32 = torch.float32
     w_type = f32 if flags & FLAG_ROPE_WEIGHT_FP32 else dtype
     rows = 0 if cos is None else cos.shape[0]
+    if rows > 0x7FFFFFFF:   # (the call takes the count in 32 bits)
+        _refuse(E_SHAPE)
     of_q, of_k, weight, table = (B, Hq, L, d), (B, Hk, L, d), (d,), (rows, rot // 2)
     sq, sk = (s[0], s[1], s[2], 1), (s[3], s[4], s[5], 1)
     given = [(q, dtype, of_q, sq), (k, dtype, of_k, sk), (q_weight, w_type, weight, None), (k_weight, w_type, weight, None),
@@ -421,6 +425,8 @@ def _scratch(workspace, device):
         return None, 0
     if workspace.get_device() != device:
         _refuse(E_DEVICE)
+    if not workspace.is_contiguous():   # (elements that share memory do not count as bytes)
+        _refuse(E_SHAPE)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 

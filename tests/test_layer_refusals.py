@@ -206,3 +206,32 @@ def test_bindings_compare_tensors_with_the_params():
     expect(F.E_DTYPE, lambda: cross(q_lens=torch.zeros(2)))
     expect(F.E_SHAPE, lambda: F.make_cross_params(q, kv, kv[:, :, :4], q, 0.1))
     expect(F.E_STRIDE, lambda: F.make_cross_params(q, kv.transpose(2, 3).contiguous().transpose(2, 3), kv, q, 0.1))
+
+
+def test_bindings_refuse_what_the_pointers_would_hide():
+    # an axis without its theta, or with more than an axis has
+    out = torch.zeros(9, 32)
+    expect(F.E_SHAPE, lambda: F.fgattn_rope_table([(9, 32)], out, out))
+    expect(F.E_SHAPE, lambda: F.fgattn_rope_table([(9, 32, 1e4, 0.0, 1.0, 1.0, 0.0, 32.0, 1.0, 1.0)], out, out))
+    # a table of 2^32 + 9 rows, which 32 bits would take for 9 (no memory behind it)
+    q = torch.zeros(1, 2, 9, 64, dtype=torch.bfloat16)
+    p = F.make_rope_params(q, None, q, None, 64)
+    many = torch.empty(2 ** 32 + 9, 32, device="meta")
+    expect(F.E_SHAPE, lambda: F.fgattn_rope_forward(q, None, p, q, None, many, many))
+    # a workspace of one element seen a million times
+    kv, lse = torch.zeros(1, 1, 9000, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 9)
+    p = F.make_cross_params(q, kv, kv, q, 0.1, q, q, kv, kv)
+    thin = torch.zeros(1, dtype=torch.uint8).expand(F.fgattn_cross_backward_workspace_bytes(p))
+    expect(F.E_SHAPE, lambda: F.fgattn_cross_forward(q, kv, kv, p, q, lse, thin))
+    expect(F.E_SHAPE, lambda: F.fgattn_cross_backward(q, kv, kv, q, lse, q, p, q, kv, kv, thin))
+    w = torch.zeros(64, dtype=torch.float32)
+    p = F.make_rope_params(q, None, q, None, 0)
+    thin = torch.zeros(1, dtype=torch.uint8).expand(F.fgattn_rope_workspace_bytes(p))
+    expect(F.E_SHAPE, lambda: F.fgattn_rope_backward(q, None, p, q, None, q, None, dq_weight=w, workspace=thin))
+
+
+def test_rope_tokens_stay_within_a_launch():
+    # 2^25 tokens of the widest rows are 2^23 workgroups of 256 threads
+    assert F.fgattn_rope_workspace_bytes(rope_params(L=2 ** 24)) > 0                  # (two batch entries)
+    assert F.fgattn_rope_workspace_bytes(rope_params(B=3, L=2 ** 24)) == 0
+    assert rope_forward(rope_params(B=3, L=2 ** 24), rows=2 ** 24) == F.E_SHAPE
