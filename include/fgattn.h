@@ -267,12 +267,12 @@ typedef struct fgattn_rope_params {
  * Queries and keys, normed per head and turned by their positions, in one pass:
  *   z = x * rsqrt(mean(x^2) + eps) * weight  (with FGATTN_FLAG_ROPE_NORM, else z = x);
  *   (y_a, y_b) = (z_a cos - z_b sin, z_b cos + z_a sin) for every pair (a, b), y = z for the elements from rot_dims on.
- * Formed in fp32, rounded once.
+ * Formed in fp32, rounded once.  An infinity or NaN reaches its own pair only, and through the norm its own row.
  *   q, k        : [B, Hq, L, d] and [B, Hk, L, d] (k may be NULL where Hk = 0), 16-byte aligned.
  *   q_weight, k_weight : [d] or NULL (weight 1); NULL without the norm flag.
  *   cos, sin    : fp32 [table_rows, rot_dims / 2], contiguous (fgattn_rope_table's, or any); NULL allowed where rot_dims = 0.
  *   positions   : int32 [B, L], the table's row of every token; NULL: token l takes row l, and table_rows >= L.  A position
- *                 outside [0, table_rows) turns nothing (as angle 0 and mscale 1 would): padding may hold -1.
+ *                 outside [0, table_rows) turns nothing, y = z: padding may hold -1.
  *   q_out, k_out: the results; each may be its input itself (same strides).
  */
 int fgattn_rope_forward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,

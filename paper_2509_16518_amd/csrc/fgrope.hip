@@ -122,6 +122,8 @@ struct RowLane {
   int other;       // PAIRS_HALF: first element of the partners' chunk
   bool active;     // e0 < d
   float c[V], s[V];
+  static constexpr int EACH = PAIRS == PAIRS_NEXT ? 2 : PAIRS == PAIRS_HALF ? V : 1;   // elements that are turned or not together
+  bool on[V / EACH];   // (lane masks in scalar registers)
 
   __device__ __forceinline__ void place(const RopeArgs& a, int lane) {
     e0 = (lane % LPR) * V;
@@ -130,7 +132,13 @@ struct RowLane {
     const int half = a.rot >> 1;
     other = e0 < half ? e0 + half : e0 < a.rot ? e0 - half : e0;
   }
-  // cosines and signed sines (y = z c + partner s) of a token; `back`: turned back
+  // y = z c + partner s, y = z where nothing is turned: the other term is left out there and not multiplied by 0, which an infinite or
+  // NaN partner would turn into NaN (adding -0 keeps every z to the bit)
+  __device__ __forceinline__ float turned(int i, float z, float partner) const {
+    const float other_term = partner * s[i];
+    return z * c[i] + (on[i / EACH] ? other_term : -0.0f);
+  }
+  // cosines and signed sines of a token; `back`: turned back
   __device__ __forceinline__ void angles(const RopeArgs& a, int row, bool back) {
     const bool turns = (unsigned)row < (unsigned)a.table_rows;
     const int half = a.rot >> 1;
@@ -141,13 +149,14 @@ struct RowLane {
       typedef float Pairs __attribute__((ext_vector_type(N), aligned(4)));
       if (PAIRS == PAIRS_HALF || e0 + V <= a.rot) {
         const int pair = PAIRS == PAIRS_NEXT ? e0 >> 1 : e0 < half ? e0 : e0 < a.rot ? e0 - half : 0;
-        const bool on = turns && e0 < a.rot;
+        const bool all = turns && e0 < a.rot;
+        for (int i = 0; i < V / EACH; i++) on[i] = all;
         Pairs cs, sn;
         for (int i = 0; i < N; i++) {
           cs[i] = 1.0f;
           sn[i] = 0.0f;
         }
-        if (on) {
+        if (all) {
           cs = *reinterpret_cast<const Pairs*>(a.cos + at + pair);
           sn = *reinterpret_cast<const Pairs*>(a.sin + at + pair);
         }
@@ -166,9 +175,10 @@ struct RowLane {
       const int e = e0 + i;
       const int pair = PAIRS == PAIRS_NEXT ? e >> 1 : e < half ? e : e - half;
       const bool first = PAIRS == PAIRS_NEXT ? (e & 1) == 0 : e < half;
-      const bool on = turns && e < a.rot;
-      c[i] = on ? a.cos[at + pair] : 1.0f;
-      const float sn = on ? a.sin[at + pair] : 0.0f;
+      const bool here = turns && e < a.rot;
+      on[i / EACH] = here;
+      c[i] = here ? a.cos[at + pair] : 1.0f;
+      const float sn = here ? a.sin[at + pair] : 0.0f;
       s[i] = first != back ? -sn : sn;
     }
   }
@@ -264,7 +274,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a) {
         if (a.norm) rstd = rsqrtf(row_sum<LPR>(r.active ? ss : 0.0f) * a.inv_d + a.eps);
         Vec res;
 #pragma unroll
-        for (int i = 0; i < V; i++) res[i] = (T)(z[i] * w[i] * rstd * r.c[i] + zp[i] * wp[i] * rstd * r.s[i]);
+        for (int i = 0; i < V; i++) res[i] = (T)r.turned(i, z[i] * w[i] * rstd, zp[i] * wp[i] * rstd);
         if (valid && h + u < h1) *reinterpret_cast<Vec*>(y + (int64_t)(h + u) * a.y_sh[t] + r.e0) = res;
       }
     }
@@ -315,8 +325,7 @@ __global__ void __launch_bounds__(kThreads) rope_grad_kernel(const RopeArgs a) {
         for (int u = 0; u < U; u++) {
           float dz[V];
 #pragma unroll
-          for (int i = 0; i < V; i++)
-            dz[i] = (float)gv[u][i] * r.c[i] + (PAIRS == PAIRS_NEXT ? (float)gv[u][i ^ 1] : (float)go[u][i]) * r.s[i];
+          for (int i = 0; i < V; i++) dz[i] = r.turned(i, (float)gv[u][i], PAIRS == PAIRS_NEXT ? (float)gv[u][i ^ 1] : (float)go[u][i]);
           const bool counts = valid && h + u < h1;
           if (a.norm) {
             float ss = 0.0f, dot = 0.0f;
