@@ -109,7 +109,7 @@ __device__ __forceinline__ void pack_rows(const f32x16& x, bf16x8 (&out)[2]) {  
 }
 
 template <int D>
-__device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int g) {
+__device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int g, int keep) {   // (`keep`: see store_row16)
 #pragma unroll
   for (int db = 0; db < D / 32; db++)
 #pragma unroll
@@ -117,7 +117,7 @@ __device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D /
       f32x4 f;
 #pragma unroll
       for (int e = 0; e < 4; e++) f[e] = acc[db][4 * r4 + e] * factor;
-      *reinterpret_cast<i32x2*>(row + 32 * db + 8 * r4 + 4 * g) = __builtin_bit_cast(i32x2, __builtin_convertvector(f, bf16x4));
+      *reinterpret_cast<i32x2*>(row + 32 * db + 8 * r4 + 4 * g) = __builtin_bit_cast(i32x2, __builtin_convertvector(f, bf16x4)) & keep;
     }
 }
 
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
               *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * r4 + 4 * g) = f32x4{acc[db][4 * r4], acc[db][4 * r4 + 1], acc[db][4 * r4 + 2], acc[db][4 * r4 + 3]};
         }
       } else {   // (zeros where the row does not count)
-        store_row16<D>(a.dq + b * a.dq_sb + head * a.dq_sh + (int64_t)pos * a.dq_sl, acc, counts ? a.scale : 0.0f, g, mine);
+        store_row16<D>(a.dq + b * a.dq_sb + head * a.dq_sh + (int64_t)pos * a.dq_sl, acc, a.scale, g, mine, counts ? -1 : 0);
       }
     }
     if constexpr (STREAM) wait_vmem_all();   // (tiles that nobody reads; none may land after this workgroup)
@@ -524,9 +524,9 @@ __global__ void __launch_bounds__(256, 2) dkdv_kernel(const BwdArgs a) {
         }
     }
   } else if (my_key < a.Lk) {
-    const bool counts = my_key < k_len;
-    store_row<D>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)my_key * a.dk_sl, dk, counts ? a.scale : 0.0f, g);
-    store_row<D>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)my_key * a.dv_sl, dv, counts ? 1.0f : 0.0f, g);
+    const int keep = my_key < k_len ? -1 : 0;   // (the accumulators behind the last key are copies of its own)
+    store_row<D>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)my_key * a.dk_sl, dk, a.scale, g, keep);
+    store_row<D>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)my_key * a.dv_sl, dv, 1.0f, g, keep);
   }
 }
 

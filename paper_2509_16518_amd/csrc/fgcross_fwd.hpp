@@ -48,8 +48,9 @@ __device__ __forceinline__ void gather16(const void* base, unsigned byte_off, un
 
 // A row of the result from a transposed accumulator (lane (g, row): elements 8 r4 + 4 g .. + 3 of every block): the lanes of a pair
 // exchange halves, so that each stores 16 bytes and a row gets 32 in a run (with 8 bytes per lane twice the stores).
+// `keep`: all ones, or 0 for a row of zeros whatever the accumulator holds (a factor of 0 would leave NaN where it overflowed).
 template <int D>
-__device__ __forceinline__ void store_row16(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int g, bool valid) {
+__device__ __forceinline__ void store_row16(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int g, bool valid, int keep = -1) {
   i32x4 out[D / 16];
 #pragma unroll
   for (int db = 0; db < D / 32; db++)
@@ -69,7 +70,7 @@ __device__ __forceinline__ void store_row16(uint16_t* row, const f32x16 (&acc)[D
     }
   if (valid) {
 #pragma unroll
-    for (int i = 0; i < D / 16; i++) *reinterpret_cast<i32x4*>(row + 16 * i + 8 * g) = out[i];
+    for (int i = 0; i < D / 16; i++) *reinterpret_cast<i32x4*>(row + 16 * i + 8 * g) = out[i] & keep;
   }
 }
 
