@@ -331,9 +331,10 @@ int fgattn_cross_forward(const void* q, const void* k, const void* v, const int3
  * Its gradients: dq, dk, dv (bf16, every element written: zeros for rows from q_lens[b] and keys from k_lens[b] on) from
  * the forward call's inputs and results and dout, the gradient of out (rows from q_lens[b] on are not read, of out and
  * lse neither).  Where query heads share a key head its gradient is the sum of theirs.  P and dS are rounded to
- * bf16 for the matrix instructions, all sums are fp32, the results are rounded once.  dS = P (dP - D): with more than 128 keys
- * D = sum dout * out is formed from the bf16 out, whose rounding shows in dq and dk where one key takes nearly all of a row's P and dS
- * nearly cancels (2.4% of dq in the worst of 1750 drawn calls, one of two rows); up to 128 keys it is the fp32 sum of P dP.  A
+ * bf16 for the matrix instructions, all sums are fp32, the results are rounded once.  dS = P (dP - D): in entries of the batch with more
+ * than 128 keys (min(k_lens[b], Lk)) D = sum dout * out is formed from the bf16 out, whose rounding shows in dq and dk where one key takes
+ * nearly all of a row's P and dS nearly cancels (2.4% of dq in the worst of 1750 drawn calls, one of two rows); in entries with up to 128
+ * keys, however far they are padded, it is the fp32 sum of P dP, and out is not read.  A
  * (batch, head) slice of q and of dout ends below 4 GiB, as one of k and v does in both calls (FGATTN_E_STRIDE).
  */
 size_t fgattn_cross_backward_workspace_bytes(const fgattn_cross_params* p);

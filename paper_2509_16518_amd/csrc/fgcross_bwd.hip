@@ -6,7 +6,8 @@
 //                (as in fgcross_fwd.hpp: one key head's K and V for all of a workgroup's tiles, or rings).  It also forms D and
 //                leaves (lse, D) of every row for the second kernel.  D comes from the bf16 result, whose rounding shows in dP - D where
 //                a row has few keys (a relative error of dQ of 0.0026 with 77 keys and 0.0036 with 3, against 0.0024 with the exact
-//                D): with up to kOwnDelta keys it is the sum of P dP over a first pass through the keys, and the result is not read.  With few rows and many keys the keys are split over
+//                D): in an entry of the batch with up to kOwnDelta keys, however far it is padded, it is the sum of P dP over a
+//                first pass through the keys, and the result is not read.  With few rows and many keys the keys are split over
 //                workgroups, whose fp32 partial sums are added up in a fixed order by a kernel of their own.
 //   dkdv_kernel  a wave owns 32 keys (K in registers, one key per lane, its V rows in LDS); the queries stream through LDS.  With few
 //                keys and many queries the query rows are split over workgroups, and the partial sums added up likewise.
@@ -34,7 +35,6 @@ struct BwdArgs {
   int32_t B, H, Hkv, group, Lq, Lk;
   int32_t n_items, KB, n_split, units, units_per_split;   // dkdv_kernel; KB: key tiles of a slice; units: 32-row tiles of a key head's rows
   int32_t rows, QB, unit, QU, dq_units, k_split, split_keys;   // dq_kernel (as CrossArgs); ranges of split_keys keys
-  int32_t own_delta;                                           // dq_kernel forms D from P and dP and does not read the result
   float scale, c_log2;
 };
 
@@ -125,6 +125,7 @@ __device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&acc)[D /
 // for its rows (the whole call for 12 heads x 32760 tokens and 512 keys of 128 elements 404 us, 412 with one of eight; 1024 keys 698, 710).
 constexpr int dq_waves(bool stream) { return stream ? 4 : 8; }
 constexpr int kDqRingBytes = kLdsBytes / 2;
+constexpr int kOwnDelta = 128;   // see the top of the file; a range of keys has at least as many (bwd_plan)
 
 // A wave's work on a query tile is a software pipeline over its key tiles: step n runs S(n+1) = K(n+1) Q^T and dP(n+1) = V(n+1) dO^T side by
 // side with the exponentials and products that make dS(n) of S(n) and dP(n), then dQ += K(n)^T dS(n)^T.  Bound: the matrix
@@ -167,6 +168,7 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
     const int k_len = a.k_lens ? max(0, min(a.k_lens[b], a.Lk)) : a.Lk;
     const int key0 = split * a.split_keys, cnt = max(0, min(k_len - key0, a.split_keys));
     const int np = (cnt + 63) >> 6;
+    const bool own_delta = k_len <= kOwnDelta;   // (all of the entry's keys are in the first range then)
     const int last = min(first + n_here * a.unit, a.QB);
     const uint16_t* kbase = a.k + b * a.k_sb + hk * a.k_sh + key0 * a.k_sl;
     const uint16_t* vbase = a.v + b * a.v_sb + hk * a.v_sh + key0 * a.v_sl;
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
           if (counts) {   // (rows that do not count may hold anything)
             qr = *reinterpret_cast<const i32x4*>(qp + (2 * s + g) * 16);
             dr = *reinterpret_cast<const i32x4*>(dp + (2 * s + g) * 16);
-            if (!a.own_delta) orow[s] = *reinterpret_cast<const i32x4*>(op + (2 * s + g) * 16);
+            if (!own_delta) orow[s] = *reinterpret_cast<const i32x4*>(op + (2 * s + g) * 16);
           }
           qf[s] = __builtin_bit_cast(bf16x8, qr);
           dof[s] = __builtin_bit_cast(bf16x8, dr);
@@ -310,7 +312,28 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
           for (int c = 0; c < 2; c++)
             acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.transposed(smem + k_at, db, c), d2[c], acc[db], 0, 0, 0);
       };
-      if (!STREAM && a.own_delta) {   // D = sum over the keys of P dP
+      int k_at = STREAM ? slot * SLOT : 0;
+      // Where the tile after the one at k_at lies.  STREAM: it has arrived (what was fetched in the SLOTS - 3 steps before may still be
+      // under way), and every wave is done with the tile before this one, into whose slot the one SLOTS - 1 ahead follows.
+      auto advance = [&](bool odd) {
+        if constexpr (STREAM) {
+          if (TILES == 2 && odd) return k_at + TB;
+          wait_vmem_le<(SLOTS - 3) * 2 * IPW>();
+          __syncthreads();
+          slot = slot + 1 == SLOTS ? 0 : slot + 1;
+          return slot * SLOT;
+        } else {
+          return k_at + SLOT;
+        }
+      };
+      auto load = [&](auto ec) {   // between the matrix instructions
+        constexpr int e = decltype(ec)::value, EVERY = NE / (2 * IPW > 0 ? 2 * IPW : 1);
+        if constexpr (STREAM && e % EVERY == 1 % EVERY && e / EVERY < 2 * IPW) fetch_kv(e / EVERY);
+      };
+      auto load_all = [&]() {
+        [&]<int... E>(std::integer_sequence<int, E...>) { (load(std::integral_constant<int, E>()), ...); }(std::make_integer_sequence<int, NE>());
+      };
+      if (own_delta) {   // D = sum over the keys of P dP
         auto sum = [&](int t, const f32x16& So, const f32x16& dPo) {
           const int limit = cnt - 32 * t - 4 * g;
 #pragma unroll
@@ -320,13 +343,18 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
           }
         };
         for (int p = 0; p < np; p++) {
-          scores(2 * p * SLOT, SA, DA, [](auto) {});
-          scores((2 * p + 1) * SLOT, SB, DB, [&](auto ec) {
+          scores(k_at, SA, DA, [](auto) {});
+          k_at = advance(true);
+          scores(k_at, SB, DB, [&](auto ec) {
             if constexpr (decltype(ec)::value == 0) sum(2 * p, SA, DA);
+            if constexpr (TILES == 1) load(ec);
           });
+          k_at = advance(false);
+          load_all();
           sum(2 * p + 1, SB, DB);
         }
         delta = lane_pair_sum(delta);
+        if constexpr (!STREAM) k_at = 0;   // (STREAM: the ring has come round to the first tile again)
       }
       if (counts && g == 0 && split == 0) {
         const f32x2 st = {lse2, delta};
@@ -337,24 +365,6 @@ __global__ void __launch_bounds__(dq_waves(STREAM) * 64, 2) dq_kernel(const BwdA
 #pragma unroll
         for (int r = 0; r < 16; r++) acc[db][r] = 0.0f;
       if (np > 0) {
-        int k_at = STREAM ? slot * SLOT : 0;
-        // Where the tile after the one at k_at lies.  STREAM: it has arrived (what was fetched in the SLOTS - 3 steps before may still be
-        // under way), and every wave is done with the tile before this one, into whose slot the one SLOTS - 1 ahead follows.
-        auto advance = [&](bool odd) {
-          if constexpr (STREAM) {
-            if (TILES == 2 && odd) return k_at + TB;
-            wait_vmem_le<(SLOTS - 3) * 2 * IPW>();
-            __syncthreads();
-            slot = slot + 1 == SLOTS ? 0 : slot + 1;
-            return slot * SLOT;
-          } else {
-            return k_at + SLOT;
-          }
-        };
-        auto load = [&](auto ec) {   // between the matrix instructions
-          constexpr int e = decltype(ec)::value, EVERY = NE / (2 * IPW > 0 ? 2 * IPW : 1);
-          if constexpr (STREAM && e % EVERY == 1 % EVERY && e / EVERY < 2 * IPW) fetch_kv(e / EVERY);
-        };
         scores(k_at, SA, DA, [](auto) {});
         for (int p = 0; p < np; p++) {
           // tile 2 p + 1 beside tile 2 p
@@ -576,8 +586,6 @@ __global__ void __launch_bounds__(256) sum_q_kernel(const BwdArgs a) {
       __builtin_bit_cast(i32x2, __builtin_convertvector(sum, bf16x4));
 }
 
-constexpr int kOwnDelta = 128;   // see the top of the file
-
 struct BwdPlan {
   int KB, units, n_split, units_per_split;                      // dkdv_kernel
   int QB, unit, QU, k_split, split_keys;                        // dq_kernel
@@ -607,7 +615,8 @@ static BwdPlan bwd_plan(const fgattn_cross_params* p, int cus) {
   s.k_split = 1;
   s.split_keys = p->Lk;
   if (p->Lk > fit) {
-    // as many ranges as make a workgroup of eight tiles for each of 256 compute units, of 128 keys or more; their partial sums stay
+    // as many ranges as make a workgroup of eight tiles for each of 256 compute units, of 128 keys or more (91 at least, as Lk > 320, in
+    // whole 64s: an entry with up to kOwnDelta keys has them in the first range); their partial sums stay
     // below 256 x 8 tiles, 34 MB (64 tokens of 8 heads, 8192 keys: the whole call 253 us in one range, 41 in 32; 24 x 1000
     // tokens, 2048 keys 134 and 125)
     int64_t ranges = 256 / (slices * ((s.QB + 7) / 8));
@@ -725,7 +734,6 @@ int fgattn_cross_backward(const void* q, const void* k, const void* v, const voi
   a.B = p->B; a.H = p->H; a.Hkv = p->Hkv; a.group = p->H / p->Hkv; a.Lq = p->Lq; a.Lk = p->Lk;
   a.rows = a.group * p->Lq; a.QB = s.QB; a.unit = s.unit; a.QU = s.QU; a.dq_units = p->B * p->Hkv * s.k_split * s.QU;
   a.k_split = s.k_split; a.split_keys = s.split_keys;
-  a.own_delta = p->Lk <= fgx::kOwnDelta;   // (one range, resident)
   a.KB = s.KB; a.n_split = s.n_split; a.units = s.units; a.units_per_split = s.units_per_split;
   a.scale = p->scale;
   a.c_log2 = p->scale * 1.44269504088896340736f;
