@@ -188,18 +188,30 @@ def check_untracked_loads(asm_path):
     return loads
 
 
+# Spilled vector registers that are tolerated in kernels that gather; none in others.  All of them are reloaded outside the loop over
+# the keys: the forward kernel's once per item, cross_kernel's once per key head.
+SPILLS = {"fgattn_fwd_kernel": 1, "cross_kernelILi128ELi8ELb1ELb1": 4, "cross_kernelILi128ELi8ELb1ELb0": 1, "cross_kernelILi128ELi8ELb0ELb1": 5,
+          "cross_kernelILi128ELi8ELb0ELb0": 6}
+
+
 def check_spills(asm_path):
-    """A forward kernel that spills vector registers reloads them through the counter its gathers are waited for with.
-    One register is tolerated (it is reloaded once per item where the key loop has no room)."""
+    """A kernel that gathers rows into LDS and spills vector registers reloads them through the counter that its gathers are waited for
+    with: each reload drains what is under way.  Holds for every kernel with such loads, and for the forward kernel in any form."""
     import re
-    name = None
+    function, name, gathers = None, None, set()
     with open(asm_path) as f:
         for line in f:
+            if line.startswith("_Z") and ":" in line:
+                function = line.split(":", 1)[0]
+            elif "global_load_lds" in line.split(";", 1)[0]:
+                gathers.add(function)
             m = re.match(r"\s+\.(name|vgpr_spill_count):\s+(\S+)", line)
             if m and m.group(1) == "name":
                 name = m.group(2)
-            elif m and "fgattn_fwd_kernel" in (name or "") and int(m.group(2)) > 1:
-                raise RuntimeError("%s: %s spills %s vector registers" % (asm_path, name, m.group(2)))
+            elif m and (name in gathers or "fgattn_fwd_kernel" in (name or "")):
+                allowed = max([n for part, n in SPILLS.items() if part in name], default=0)
+                if int(m.group(2)) > allowed:
+                    raise RuntimeError("%s: %s spills %s vector registers, %d at most" % (asm_path, name, m.group(2), allowed))
 
 
 def check_rounding_mode(asm_path):
