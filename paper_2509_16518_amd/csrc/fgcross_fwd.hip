@@ -160,9 +160,13 @@ static Plan plan_of(const fgattn_cross_params* p, int cus) {
   // against 26.7.  More keys: 512 keys 8 x 256 tokens 12.4 against 10.6, 12 x 512 15.6 against 18.4; 2048 keys 8 x 64 tokens 12.7
   // against 11.5, 8 x 256 17.8 against 22.8; 8192 keys 8 x 256 tokens 32 against 26, 12 x 512 49 against 69.  With d = 64 twice
   // as many single waves are resident: 2048 keys 24 x 1000 tokens 44 against 32, 8192 keys 12 x 4096 tokens 145 against 162.
+  // With few tiles to a key head most waves of a workgroup go along with the keys for nothing, however many key heads there are:
+  // d = 128, one tile 2048 keys 160 heads 50 against 33, 8192 keys 512 heads 520 against 377; two 8192 keys 256 heads 273 against 220; three
+  // 2048 keys 256 heads 74 against 86, 8192 keys 64 heads 72 against 84.  d = 64, one 1280 heads 2048 keys 225 against 121; five 260 heads
+  // 83 against 53; six 240 heads 47 against 47, to 8192 keys 177 against 204.
   if (!s.stream) s.tiles = p->Lk <= 160 ? tiles * p->d >= 128 * 1024 : true;
-  else if (p->d == 64) s.tiles = tiles >= 1280;
-  else s.tiles = tiles * tiles >= p->Lk && tiles * p->Lk >= 65536;
+  else if (p->d == 64) s.tiles = tiles >= 1280 && s.QB >= 6;
+  else s.tiles = tiles * tiles >= p->Lk && tiles * p->Lk >= 65536 && s.QB >= 3;
   s.n_split = 1;
   s.split_keys = p->Lk;
   const int waves_fit = p->d == 64 ? kWaves64 : kWaves128;
