@@ -229,7 +229,13 @@ static int launch_tiles(const CrossArgs& a, bool rings, int lds, int cus, hipStr
   constexpr int WV = D == 64 ? kWaves64 : kWaves128;
   if (rings)
     return a.n_split > 1 ? launch_cross<D, kWavesRings, true, true>(a, lds, cus, stream) : launch_cross<D, kWavesRings, true, false>(a, lds, cus, stream);
-  return a.n_split > 1 ? launch_cross<D, WV, false, true>(a, lds, cus, stream) : launch_cross<D, WV, false, false>(a, lds, cus, stream);
+  // Parts of resident keys: d = 128 only.  With d = 64 there are two ranges at most, of more keys than LDS holds: plan_of asks for 1280
+  // tiles, which are more than 106 units of twelve, and splits them from 2012 keys on.
+  if (a.n_split > 1) {
+    if constexpr (D == 128) return launch_cross<D, WV, false, true>(a, lds, cus, stream);
+    return FGATTN_E_SHAPE;
+  }
+  return launch_cross<D, WV, false, false>(a, lds, cus, stream);
 }
 
 template <int D>
