@@ -317,6 +317,9 @@ typedef struct fgattn_cross_params {
  *   q_lens, k_lens : int32 [B] or NULL (all tokens / all keys); values are taken into [0, Lq] and [0, Lk].
  *            Keys from k_lens[b] on are not read, whatever they hold; rows of out and lse from q_lens[b] on are not written.
  *            No keys: out = 0, lse = -inf.
+ * Scores, maxima, exponentials and all sums (lse from the exponentials as they are) are fp32; P is rounded to bf16 for the matrix
+ * instructions that form P V, out once: a root mean square error of out of 0.0023 relative to its size, where the rounding of an exact
+ * result gives 0.0017.
  * `workspace`: at least fgattn_cross_workspace_bytes(p) bytes, 256-byte aligned; NULL where that is 0.  (Calls with few rows
  * split the keys over the chip and join the parts there.)
  */

@@ -7,7 +7,8 @@
 //                leaves (lse, D) of every row for the second kernel.  D comes from the bf16 result, whose rounding shows in dP - D where
 //                a row has few keys (a relative error of dQ of 0.0026 with 77 keys and 0.0036 with 3, against 0.0024 with the exact
 //                D): in an entry of the batch with up to kOwnDelta keys, however far it is padded, it is the sum of P dP over a
-//                first pass through the keys, and the result is not read.  With few rows and many keys the keys are split over
+//                first pass through the keys, and the result is not read.  (With more keys that pass would add 16 matrix instructions
+//                per tile to the 24; what is left is an error of up to 2.4% of dQ where one key takes nearly all of a row's P.)  With few rows and many keys the keys are split over
 //                workgroups, whose fp32 partial sums are added up in a fixed order by a kernel of their own.
 //   dkdv_kernel  a wave owns 32 keys (K in registers, one key per lane, its V rows in LDS); the queries stream through LDS.  With few
 //                keys and many queries the query rows are split over workgroups, and the partial sums added up likewise.

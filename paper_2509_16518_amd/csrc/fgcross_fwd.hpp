@@ -8,6 +8,10 @@
 // exponentials of S(n), where n+1 may be the first key tile of the next query tile, whose rows have been loaded meanwhile, and n-1 the
 // last one of the tile before, whose result is then stored.  With 8 key tiles per query tile, starting and ending a pipeline for each
 // took 7.2 of 15.6 us.
+//
+// P is rounded to bf16, the type of V and so of both operands of the matrix instruction that forms P V; the sums beside it take P as it is.
+// The relative root mean square error of a result is 0.0023 (512 and 256 keys), 0.0017 with exact P.  P in two bf16 parts would make three
+// matrix products of two, in a kernel that the matrix pipe bounds.
 #pragma once
 #include "fgattn_fwd.hpp"
 
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       l_run2 = l_new2;
     };
     // Where the next two steps find their tiles: V's pair p and K's pair p + 1, or of the next query tile's first.  STREAM: K(p+1) and
-    // V(p) have arrived (what was fetched in the three rounds before this one may still be under way), every wave is
+    // V(p) have arrived (what was fetched in the SLOTS - 2 rounds before this one may still be under way), every wave is
     // done with K(p) and V(p-1), and the pairs SLOTS and SLOTS - 1 ahead follow into their slots.
     int k_at = 0, v_at = V_OFF;
     bool v_first = true;
