@@ -315,7 +315,8 @@ typedef struct fgattn_cross_params {
  * out = softmax(scale * Q K^T) V over the first k_lens[b] keys, lse = ln sum exp(scale * q.k) over them.
  *   q, out : bf16 [B, H, Lq, d];  k, v : bf16 [B, Hkv, Lk, d];  lse : fp32 [B, H, Lq] contiguous.
  *   q_lens, k_lens : int32 [B] or NULL (all tokens / all keys); values are taken into [0, Lq] and [0, Lk].
- *            Keys from k_lens[b] on are not read, whatever they hold; rows of out and lse from q_lens[b] on are not written.
+ *            Keys from k_lens[b] on are not read, whatever they hold, nor rows of q from q_lens[b] on (but the first where there is
+ *            none); rows of out and lse from q_lens[b] on are not written.
  *            No keys: out = 0, lse = -inf.
  * Scores, maxima, exponentials and all sums (lse from the exponentials as they are) are fp32; P is rounded to bf16 for the matrix
  * instructions that form P V, out once: a root mean square error of out of 0.0023 relative to its size, where the rounding of an exact

@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
       my_row = tile * a.tile_rows + (qg - my_member * a.tile_rows);
       my_row_valid = tile >= 0 && my_row < a.L;
     }
-    int my_head = h, my_pos = my_row;   // CROSS: this lane's query head and token
+    int my_head = h, my_pos = my_row, q_pos = my_row;   // CROSS: this lane's query head and token, and the token whose row it reads
     int key0 = 0;                       // CROSS: the first key of the item's range
     if constexpr (CROSS) {
       const int row = min(my_row, a.L - 1), of_group = (int)((unsigned)row / (unsigned)a.Lq);
@@ -411,6 +411,7 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
       my_pos = row - of_group * a.Lq;
       const int q_len = a.q_lens ? max(0, min(a.q_lens[b], a.Lq)) : a.Lq;
       my_row_valid &= my_pos < q_len;
+      q_pos = min(my_pos, max(q_len - 1, 0));   // (as in cross_kernel)
       const int first_of = row0 / a.Lq;   // (an item of nothing but rows past the end of its sequence)
       if (first_of == (row_end - 1) / a.Lq && row0 - first_of * a.Lq >= q_len) break;
     }
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(WV * 64, OCC) fgattn_fwd_kernel(const FwdArgs 
     bf16x8 qf[C::SSTEPS];
     {
       int qrow = GROUPED ? (my_row_valid ? my_row : 0) : min(my_row, a.L - 1);
-      if constexpr (CROSS) qrow = my_pos;
+      if constexpr (CROSS) qrow = q_pos;
       const char* qp = reinterpret_cast<const char*>(a.q + b * a.q_sb + (CROSS ? my_head : h) * a.q_sh + (int64_t)qrow * a.q_sl);
 #pragma unroll
       for (int s = 0; s < C::SSTEPS; s++) {

@@ -179,10 +179,13 @@ __global__ void __launch_bounds__(WV * 64, WV / 4) cross_kernel(const CrossArgs 
       pos = row - head * a.Lq;
       return jj * 32 + ln < a.rows && pos < q_len && (!STREAM || jj < last);
     };
+    // (Rows behind the sequence are read as its last one, whatever they hold: the rows of a tile move their exponent bases together, so
+    // theirs would show in the last bits of the others.)
+    const int last_pos = max(q_len - 1, 0);
     auto load_q = [&](int jj) {
       int head, pos;
       place(jj, head, pos);
-      const char* qp = reinterpret_cast<const char*>(qbase + head * a.q_sh + (int64_t)pos * a.q_sl) + 16 * g;
+      const char* qp = reinterpret_cast<const char*>(qbase + head * a.q_sh + (int64_t)min(pos, last_pos) * a.q_sl) + 16 * g;
 #pragma unroll
       for (int s = 0; s < SSTEPS; s++) qn[s] = *reinterpret_cast<const i32x4*>(qp + 32 * s);
     };
