@@ -317,7 +317,8 @@ typedef struct fgattn_cross_params {
  *   q_lens, k_lens : int32 [B] or NULL (all tokens / all keys); values are taken into [0, Lq] and [0, Lk].
  *            Keys from k_lens[b] on are not read, whatever they hold, nor rows of q from q_lens[b] on (but the first where there is
  *            none); rows of out and lse from q_lens[b] on are not written.
- *            No keys: out = 0, lse = -inf.
+ *            No keys: out = 0, lse = -inf.  (Infinities among the counted values give infinities or NaN in out: those of the last key may
+ *            be multiplied by the probabilities 0 behind it.)
  * Scores, maxima, exponentials and all sums (lse from the exponentials as they are) are fp32; P is rounded to bf16 for the matrix
  * instructions that form P V, out once: a root mean square error of out of 0.0023 relative to its size, where the rounding of an exact
  * result gives 0.0017.
